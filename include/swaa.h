@@ -393,11 +393,181 @@ int swaa_attn_bwd(const void *q, const void *k, const void *v, const void *out, 
  */
 long long swaa_attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int N, int D, int window, int n_sink, int n_prompt);
 
+/*
+ * ---- The key/value cache's other calls: its rows are made (swaa_qk_norm_rope) for the attention calls above, and the lightest of
+ * them leave it again (swaa_attn_key_weights, swaa_cache_evict). ----
+ *
+ * RMS norms of the heads of queries and keys, and the rotation by their positions, in one pass -- what stands between the
+ * projections of a layer and its attention call -- with the keys and values of new tokens going straight into the cache that
+ * swaa_attn_decode_ex and swaa_attn_fwd_ex read.  For a row x of D elements at position pos, weights w and R = rot_dim:
+ *
+ *     n_i = x_i / sqrt(mean_j x_j^2 + eps) * w_i                               (n = x without weights)
+ *     y_a = n_a cos t - n_c sin t,  y_c = n_c cos t + n_a sin t,  t = pos * inv_freq[i]
+ *           (a, c) = (i, i + R/2), or (2 i, 2 i + 1) if interleaved, for i in [0, R/2)
+ *     y_i = n_i                                                                for i >= R
+ *
+ * Angles are taken in 64 bits, norms and products in fp32 (the squares of a row must not overflow it), and y is rounded once.
+ *
+ *   q, k          [Hq heads] and [Hkv heads] of Nq rows; read only
+ *   v             Hkv heads of Nq rows, copied to v_out; ptr NULL: no values, v_out unused
+ *   q_out         as q; the same tensor as q (pointer and strides) or one that does not overlap it
+ *   k_out, v_out  the cache: Hkv heads of Nk rows (strided, packed or paged), of which the new tokens' are written; without a
+ *                 cache (Nk = Nq, no seq_lens) the results' own rows, which may then be k and v themselves
+ *   The sequences are those of swaa_attn_fwd_ex and swaa_attn_decode_ex: row r of sequence b is the token in row
+ *   Nk_b - Nq_b + r of its cache, and row r of its q, k, v.  Fixed-length batches: Nq_b = Nq, Nk_b = seq_lens[b] clamped to
+ *   [Nq, Nk] (seq_lens NULL: Nk).  Packed batches: both offsets given, as in swaa_fwd_args (total_rows_q too); seq_lens must be
+ *   NULL.  Paged caches: as there, with pages of any size; a row whose page number lies outside the cache is not written.
+ *   positions     device ints, [B, Nq] contiguous or one per row of the packed tensors, or NULL: the row in the cache.  (They
+ *                 differ behind an eviction: tokens have left the cache, positions go on.)
+ *   q_weight, k_weight  device fp32 [D], or both NULL: no norm; eps finite and > 0 (not looked at without weights)
+ *   inv_freq      device fp32 [rot_dim / 2]; rot_dim a multiple of 16 up to D; 0: no rotation, inv_freq unused
+ *   D             a multiple of 32 up to 256; strides, alignment and dtype as in swaa_fwd_args
+ *
+ * Two new tokens must not stand in the same row of the cache.  Returns SWAA_OK or a negative swaa_status.
+ */
+typedef struct swaa_norm_rope_args {
+    swaa_tensor q, k, v;             /* read only */
+    swaa_tensor q_out, k_out, v_out; /* written */
+    int B, Hq, Hkv, D;
+    int Nq, Nk;
+    const int *cu_seqlens_q, *cu_seqlens_k; /* device, B + 1 ints each, or NULL */
+    const int *seq_lens;                    /* device, B ints, or NULL */
+    const int *positions;
+    const float *q_weight, *k_weight;
+    float eps;
+    const float *inv_freq;
+    int rot_dim;
+    int interleaved; /* 0: pairs of halves, 1: of neighbours */
+    int dtype;
+    const int *block_table; /* device, B rows of block_table_stride ints, or NULL */
+    int block_table_stride, page_size, num_pages;
+    long long total_rows_q;
+    void *stream;
+} swaa_norm_rope_args;
+
+int swaa_qk_norm_rope(const swaa_norm_rope_args *args);
+
+/*
+ * Backward pass of swaa_qk_norm_rope (sequences of one length, no cache): from the gradients of its results -- dq and dk of
+ * swaa_attn_bwd -- those of q, k and the weights.  With g the gradient dy rotated by -t, s = 1 / sqrt(mean(x^2) + eps):
+ *
+ *     dx_i = s (w_i g_i - x_i s^2 mean_j(x_j w_j g_j)),   dw_i = sum over rows of g_i x_i s       (without weights: dx = g)
+ *
+ *   q, k            the forward call's inputs; read only (not looked at without weights)
+ *   dq_out, dk_out  gradients with respect to q_out and k_out; read only
+ *   dq, dk          written; each the same tensor as the gradient it comes from (pointer and strides) or one that overlaps none
+ *                   of the others
+ *   dq_weight, dk_weight  device fp32 [D], written; unused without weights.  Sums are fp32 and taken in a fixed order: a call
+ *                   repeated gives the same bits.
+ *   N               rows of a sequence; positions device ints [B, N] or NULL: the row
+ *   workspace       device scratch memory owned by the caller, 16-byte aligned, at least
+ *                   swaa_qk_norm_rope_bwd_workspace_bytes(args) bytes (0 without weights: it may be NULL then); calls that may
+ *                   overlap on the device need separate workspaces
+ */
+typedef struct swaa_norm_rope_bwd_args {
+    swaa_tensor q, k, dq_out, dk_out; /* read only */
+    swaa_tensor dq, dk;               /* written */
+    int B, Hq, Hkv, D, N;
+    const int *positions;
+    const float *q_weight, *k_weight;
+    float eps;
+    const float *inv_freq;
+    int rot_dim, interleaved, dtype;
+    float *dq_weight, *dk_weight;
+    void *workspace;
+    long long workspace_bytes;
+    void *stream;
+} swaa_norm_rope_bwd_args;
+
+int swaa_qk_norm_rope_bwd(const swaa_norm_rope_bwd_args *args);
+
+/* Bytes of workspace swaa_qk_norm_rope_bwd needs: reads the shape fields and whether there are weights.  Host-only arithmetic. */
+long long swaa_qk_norm_rope_bwd_workspace_bytes(const swaa_norm_rope_bwd_args *args);
+
+/*
+ * The attention weight that each key has got from the query rows of an attention call, whose q, k, lse and mask these are: with
+ * Vis(r) as in swaa_fwd_args,
+ *
+ *     weights[b, g, j] = decay * weights[b, g, j] + sum_{h reads g} sum_{r : j in Vis(r)} exp(scale <q[b,h,r], k[b,g,j]> - lse[b,h,r])
+ *
+ * for j in [0, Nk_b); entries behind are left as they are.  With decay 0 what stood there is not read.  A row whose lse is
+ * -infinity adds nothing; a key gets nothing from rows that do not see it, whatever the two hold.
+ *
+ *   q, k       read only; sequences, strides, alignment, head dimensions, dtype as in swaa_norm_rope_args (q its q, k its k_out);
+ *              page numbers outside the cache are clamped to it
+ *   lse        device fp32, rows contiguous, as in swaa_fwd_args
+ *   weights    device fp32, weights[b * weights_stride_b + g * weights_stride_h + j], sequences one by one in packed batches, too
+ *   decay      finite and >= 0
+ *   workspace  device scratch memory owned by the caller, 16-byte aligned, at least swaa_attn_key_weights_workspace_bytes(args)
+ *              bytes (it may be NULL if that is 0); calls that may overlap on the device need separate workspaces
+ *
+ * Sums are fp32 and taken in a fixed order: a call repeated gives the same bits.  Returns SWAA_OK or a negative swaa_status.
+ */
+typedef struct swaa_key_weights_args {
+    swaa_tensor q, k;
+    const float *lse;
+    long long lse_stride_b, lse_stride_h;
+    float *weights;
+    long long weights_stride_b, weights_stride_h;
+    int B, Hq, Hkv, D;
+    int Nq, Nk;
+    const int *cu_seqlens_q, *cu_seqlens_k;
+    const int *seq_lens;
+    int window, n_sink, n_prompt;
+    const int *n_prompts;
+    float scale, decay;
+    int dtype;
+    const int *block_table;
+    int block_table_stride, page_size, num_pages;
+    void *workspace;
+    long long workspace_bytes;
+    void *stream;
+} swaa_key_weights_args;
+
+int swaa_attn_key_weights(const swaa_key_weights_args *args);
+
+/* Bytes of workspace swaa_attn_key_weights needs: reads the shape fields (B, Hq, Hkv, D, Nq, Nk).  Host-only arithmetic. */
+long long swaa_attn_key_weights_workspace_bytes(const swaa_key_weights_args *args);
+
+/*
+ * Eviction from a cache: every sequence longer than n_keep tokens is cut to n_keep rows, for each KV head by itself.  Its first
+ * n_sink rows stay, its last n_recent, and of those between the heaviest by `weights` (equal weights: the first; -0 is 0; what is
+ * not a number weighs most).  The rows that stay close up in their order in rows 0 .. n_keep - 1 of k and v, in place, and their
+ * weights with them; weights n_keep .. len - 1 become 0, so that the tokens that follow start there; rows n_keep .. len - 1 of k
+ * and v mean nothing.  Sequences of at most n_keep tokens keep everything.
+ *
+ *   k, v       the cache: [B, Hkv, Nk, D] with strides, or paged (a table of pages per sequence; a page belongs to one sequence
+ *              only -- pages that several share must be copied first -- and page numbers outside the cache are read clamped, not
+ *              written); 16-bit elements of either type
+ *   weights    device fp32, as in swaa_attn_key_weights
+ *   seq_lens   device, B ints, clamped to [0, Nk], or NULL: every sequence holds Nk tokens
+ *   kept       device ints [B, Hkv, n_keep], contiguous, written: the rows that stayed, ascending; -1 behind a shorter sequence's
+ *   new_lens   device, B ints, written: min(len, n_keep), the new number of cached tokens; may be seq_lens itself, or NULL
+ *   n_keep >= 1; n_sink, n_recent >= 0 with n_sink + n_recent <= n_keep
+ *
+ * The rows of a sequence no longer stand at their positions: attention over it takes window >= Nk, and new tokens pass their
+ * positions to swaa_qk_norm_rope.  Returns SWAA_OK or a negative swaa_status.
+ */
+typedef struct swaa_evict_args {
+    swaa_tensor k, v;
+    float *weights;
+    long long weights_stride_b, weights_stride_h;
+    const int *seq_lens;
+    int *kept, *new_lens;
+    int B, Hkv, D, Nk;
+    int n_keep, n_sink, n_recent;
+    const int *block_table;
+    int block_table_stride, page_size, num_pages;
+    void *stream;
+} swaa_evict_args;
+
+int swaa_cache_evict(const swaa_evict_args *args);
+
 /* Static description of a status code; never NULL, never freed. */
 const char *swaa_status_string(int status);
 
 /* Version, major * 10000 + minor * 100 + patch, of this header (raised whenever a struct or a signature changes) and of the library. */
-#define SWAA_VERSION 131
+#define SWAA_VERSION 132
 int swaa_version(void);
 
 #ifdef __cplusplus

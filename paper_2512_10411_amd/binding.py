@@ -33,6 +33,8 @@ EXPORTS = ("swaa_attn_fwd", "swaa_attn_fwd_fa_decode", "swaa_attn_fwd_ex", "swaa
            "swaa_attn_fwd_ex_workspace_bytes", "swaa_visible_pairs",
            "swaa_visible_pairs_fa_decode",
            "swaa_attn_decode", "swaa_attn_decode_ex", "swaa_attn_decode_workspace_bytes", "swaa_attn_decode_ex_workspace_bytes", "swaa_attn_decode_static", "swaa_attn_bwd", "swaa_attn_bwd_workspace_bytes",
+           "swaa_qk_norm_rope", "swaa_qk_norm_rope_bwd", "swaa_qk_norm_rope_bwd_workspace_bytes",
+           "swaa_attn_key_weights", "swaa_attn_key_weights_workspace_bytes", "swaa_cache_evict",
            "swaa_status_string", "swaa_version")
 
 _lib = None
@@ -67,6 +69,58 @@ class SwaaDecodeArgs(ctypes.Structure):
                 ("Nk", ctypes.c_int), ("D", ctypes.c_int), ("window", ctypes.c_int), ("n_sink", ctypes.c_int),
                 ("scale", ctypes.c_float), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_longlong),
                 ("stream", ctypes.c_void_p), ("dtype", ctypes.c_int)]
+
+
+class SwaaNormRopeArgs(ctypes.Structure):
+    """swaa_norm_rope_args of include/swaa.h."""
+    _fields_ = [("q", SwaaTensor), ("k", SwaaTensor), ("v", SwaaTensor),
+                ("q_out", SwaaTensor), ("k_out", SwaaTensor), ("v_out", SwaaTensor),
+                ("B", ctypes.c_int), ("Hq", ctypes.c_int), ("Hkv", ctypes.c_int), ("D", ctypes.c_int),
+                ("Nq", ctypes.c_int), ("Nk", ctypes.c_int),
+                ("cu_seqlens_q", ctypes.c_void_p), ("cu_seqlens_k", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("inv_freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("block_table", ctypes.c_void_p), ("block_table_stride", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("num_pages", ctypes.c_int), ("total_rows_q", ctypes.c_longlong), ("stream", ctypes.c_void_p)]
+
+
+class SwaaNormRopeBwdArgs(ctypes.Structure):
+    """swaa_norm_rope_bwd_args of include/swaa.h."""
+    _fields_ = [("q", SwaaTensor), ("k", SwaaTensor), ("dq_out", SwaaTensor), ("dk_out", SwaaTensor),
+                ("dq", SwaaTensor), ("dk", SwaaTensor),
+                ("B", ctypes.c_int), ("Hq", ctypes.c_int), ("Hkv", ctypes.c_int), ("D", ctypes.c_int), ("N", ctypes.c_int),
+                ("positions", ctypes.c_void_p), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("inv_freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("dq_weight", ctypes.c_void_p), ("dk_weight", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_longlong), ("stream", ctypes.c_void_p)]
+
+
+class SwaaKeyWeightsArgs(ctypes.Structure):
+    """swaa_key_weights_args of include/swaa.h."""
+    _fields_ = [("q", SwaaTensor), ("k", SwaaTensor),
+                ("lse", ctypes.c_void_p), ("lse_stride_b", ctypes.c_longlong), ("lse_stride_h", ctypes.c_longlong),
+                ("weights", ctypes.c_void_p), ("weights_stride_b", ctypes.c_longlong), ("weights_stride_h", ctypes.c_longlong),
+                ("B", ctypes.c_int), ("Hq", ctypes.c_int), ("Hkv", ctypes.c_int), ("D", ctypes.c_int),
+                ("Nq", ctypes.c_int), ("Nk", ctypes.c_int),
+                ("cu_seqlens_q", ctypes.c_void_p), ("cu_seqlens_k", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+                ("window", ctypes.c_int), ("n_sink", ctypes.c_int), ("n_prompt", ctypes.c_int), ("n_prompts", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("decay", ctypes.c_float), ("dtype", ctypes.c_int),
+                ("block_table", ctypes.c_void_p), ("block_table_stride", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("num_pages", ctypes.c_int),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_longlong), ("stream", ctypes.c_void_p)]
+
+
+class SwaaEvictArgs(ctypes.Structure):
+    """swaa_evict_args of include/swaa.h."""
+    _fields_ = [("k", SwaaTensor), ("v", SwaaTensor),
+                ("weights", ctypes.c_void_p), ("weights_stride_b", ctypes.c_longlong), ("weights_stride_h", ctypes.c_longlong),
+                ("seq_lens", ctypes.c_void_p), ("kept", ctypes.c_void_p), ("new_lens", ctypes.c_void_p),
+                ("B", ctypes.c_int), ("Hkv", ctypes.c_int), ("D", ctypes.c_int), ("Nk", ctypes.c_int),
+                ("n_keep", ctypes.c_int), ("n_sink", ctypes.c_int), ("n_recent", ctypes.c_int),
+                ("block_table", ctypes.c_void_p), ("block_table_stride", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("num_pages", ctypes.c_int), ("stream", ctypes.c_void_p)]
 
 
 class SwaaError(RuntimeError):
@@ -122,6 +176,13 @@ def load_library() -> ctypes.CDLL:
         ctypes.c_float, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_void_p]
     lib.swaa_attn_bwd_workspace_bytes.restype = ctypes.c_longlong
     lib.swaa_attn_bwd_workspace_bytes.argtypes = [ctypes.c_int] * 8
+    for name, block in (("qk_norm_rope", SwaaNormRopeArgs), ("qk_norm_rope_bwd", SwaaNormRopeBwdArgs),
+                        ("attn_key_weights", SwaaKeyWeightsArgs), ("cache_evict", SwaaEvictArgs)):
+        call = getattr(lib, "swaa_" + name)
+        call.restype, call.argtypes = ctypes.c_int, [ctypes.POINTER(block)]
+    for name, block in (("qk_norm_rope_bwd", SwaaNormRopeBwdArgs), ("attn_key_weights", SwaaKeyWeightsArgs)):
+        call = getattr(lib, f"swaa_{name}_workspace_bytes")
+        call.restype, call.argtypes = ctypes.c_longlong, [ctypes.POINTER(block)]
     lib.swaa_status_string.restype = ctypes.c_char_p
     lib.swaa_status_string.argtypes = [ctypes.c_int]
     lib.swaa_version.restype = ctypes.c_int
@@ -752,3 +813,357 @@ def swaa_attn_decode_ex(q, k, v, window: int, n_sink: int, scale: float | None =
     if rc != SWAA_OK:
         raise SwaaError(rc, swaa_status_string(rc))
     return out, lse
+
+
+# ---- the cache's other calls: its rows are made, weighed and evicted ----
+def _elements(tc, t, name, like=None, heads=None, dims=4):
+    """Raises what is wrong with a tensor of 16-bit rows, if anything is."""
+    if t.dtype is not tc.bfloat16 and t.dtype is not tc.float16:
+        raise TypeError(f"{name} must be bfloat16 or float16")
+    if not t.is_cuda or t.dim() != dims or t.stride(-1) != 1:
+        raise ValueError(f"{name} must be a GPU tensor view with {dims} dimensions and a contiguous last one")
+    if like is not None and (t.dtype is not like.dtype or t.get_device() != like.get_device() or t.shape[-1] != like.shape[-1]):
+        raise ValueError(f"{name} must have the type, device and head dimension of the others")
+    if heads is not None and t.shape[-3] != heads:
+        raise ValueError(f"{name} must have {heads} heads")
+
+
+def _numbers(tc, t, name, dtype, shape, like):
+    """Address of a contiguous tensor of 32-bit numbers of this shape on like's device, None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != like.get_device() or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {str(dtype)[6:]} tensor of shape {shape} on the GPU of the others")
+    return t.data_ptr()
+
+
+def _rows(t):
+    """swaa_tensor of a [blocks, heads, rows, D] or [heads, rows, D] view (a dimension of one entry has no stride to speak of)."""
+    n, st = t.shape, t.stride()
+    if len(n) == 3:
+        return SwaaTensor(t.data_ptr(), 0, st[0] if n[0] > 1 else 0, st[1] if n[1] > 1 else max(n[2], 1))
+    return SwaaTensor(t.data_ptr(), st[0] if n[0] > 1 else 0, st[1] if n[1] > 1 else 0, st[2] if n[2] > 1 else max(n[3], 1))
+
+
+def _fill_pages(tc, a, cache, block_table, B):
+    """The argument block's fields of a paged cache [num_pages, Hkv, page_size, D], if it is one."""
+    if block_table is None:
+        return
+    if block_table.dtype is not tc.int32 or block_table.dim() != 2 or block_table.shape[0] != B \
+            or (block_table.shape[1] > 1 and block_table.stride(1) != 1) or block_table.get_device() != cache.get_device():
+        raise ValueError("block_table must be an int32 [B, pages_per_seq] GPU tensor with contiguous rows")
+    a.block_table = block_table.data_ptr()
+    a.block_table_stride = block_table.stride(0) if B > 1 else block_table.shape[1]
+    a.num_pages, a.page_size = cache.shape[0], cache.shape[2]
+
+
+def _fill_sequences(tc, a, q, rows_of_cache, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k, seq_lens, paged):
+    """B, Nq, Nk and the lengths of a call with query rows q ([B, H, Nq, D], packed [H, Tq, D]); rows_of_cache: of a contiguous cache."""
+    packed = cu_seqlens_q is not None
+    if packed:
+        if cu_seqlens_k is None or max_seqlen_q is None or max_seqlen_k is None:
+            raise ValueError("packed batches need cu_seqlens_q, cu_seqlens_k, max_seqlen_q and max_seqlen_k")
+        n = cu_seqlens_q.numel()
+        a.cu_seqlens_q = _numbers(tc, cu_seqlens_q, "cu_seqlens_q", tc.int32, (n,), q)
+        a.cu_seqlens_k = _numbers(tc, cu_seqlens_k, "cu_seqlens_k", tc.int32, (n,), q)
+        a.B, a.Nq, a.Nk = n - 1, int(max_seqlen_q), int(max_seqlen_k)
+        if seq_lens is not None:
+            raise ValueError("packed batches have their lengths from cu_seqlens_k: no seq_lens")
+        return
+    if cu_seqlens_k is not None:
+        raise ValueError("packed batches need cu_seqlens_q, cu_seqlens_k, max_seqlen_q and max_seqlen_k")
+    if paged and max_seqlen_k is None:
+        raise ValueError("a paged cache needs max_seqlen_k")
+    a.B, a.Nq = q.shape[0], q.shape[2]
+    a.Nk = rows_of_cache if max_seqlen_k is None else int(max_seqlen_k)
+    if not paged and a.Nk > rows_of_cache:
+        raise ValueError("max_seqlen_k is more than the cache has rows")
+    a.seq_lens = _numbers(tc, seq_lens, "seq_lens", tc.int32, (a.B,), q)
+
+
+def _call(name, a):
+    """The C call `name` on a filled argument block."""
+    rc = getattr(_lib or load_library(), name)(ctypes.byref(a))
+    if rc != SWAA_OK:
+        raise SwaaError(rc, swaa_status_string(rc))
+
+
+def _scratch(tc, name, a, workspace, device):
+    """Fills in the workspace of a call, allocated here if the caller has none (kept alive by the caller of this)."""
+    need = int(getattr(_lib or load_library(), name + "_workspace_bytes")(ctypes.byref(a)))
+    if need < 0:
+        raise SwaaError(need, swaa_status_string(need))
+    if workspace is None and need > 0:
+        workspace = tc.empty(need, dtype=tc.uint8, device=device)
+    elif workspace is not None and (workspace.dtype is not tc.uint8 or not workspace.is_cuda or not workspace.is_contiguous()
+                                    or workspace.get_device() != device.index):
+        raise ValueError("workspace must be a contiguous uint8 tensor on the GPU of the others")
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    return workspace
+
+
+def _fill_norm_rope(tc, a, q, k, inv_freq, q_weight, k_weight, eps, interleaved):
+    D = q.shape[-1]
+    a.Hq, a.Hkv, a.D = q.shape[-3], k.shape[-3], D
+    if (q_weight is None) != (k_weight is None):
+        raise ValueError("q_weight and k_weight are given both or neither")
+    a.q_weight = _numbers(tc, q_weight, "q_weight", tc.float32, (D,), q)
+    a.k_weight = _numbers(tc, k_weight, "k_weight", tc.float32, (D,), q)
+    a.eps, a.interleaved = float(eps), int(bool(interleaved))
+    if inv_freq is not None:
+        a.inv_freq = _numbers(tc, inv_freq, "inv_freq", tc.float32, (inv_freq.numel(),), q)
+        a.rot_dim = 2 * inv_freq.numel()
+    a.dtype = SWAA_F16 if q.dtype is tc.float16 else SWAA_BF16
+
+
+def swaa_qk_norm_rope(q, k, inv_freq=None, positions=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                      interleaved: bool = False, v=None, q_out=None, k_out=None, v_out=None, cu_seqlens_q=None,
+                      cu_seqlens_k=None, max_seqlen_q: int | None = None, max_seqlen_k: int | None = None, seq_lens=None,
+                      block_table=None, total_rows_q: int | None = None, stream=None):
+    """RMS norms of the heads of q and k and the rotation by position, in one pass; the keys and values may go into a cache.
+
+    q [B, Hq, Nq, D], k (and v) [B, Hkv, Nq, D]: bf16 or fp16 views whose last dimension is contiguous (a [B, N, H, D]
+    projection is passed as ``t.permute(0, 2, 1, 3)``); packed batches: [H, Tq, D] with cu_seqlens_q, cu_seqlens_k and
+    the largest lengths, as in swaa_attn_fwd_ex.  q_weight, k_weight: fp32 [D], or both None for no norm.
+    inv_freq: fp32 [R / 2] frequencies of the first R dimensions (a multiple of 16), in pairs of halves or, if `interleaved`, of
+    neighbours; None: no rotation.  positions: int32 [B, Nq] (packed [Tq]) or None for the rows of the cache.
+
+    Without a cache the results are new contiguous tensors (q_out, k_out: others, q and k themselves among them).
+    With one, k_out and v_out are the cache: [B, Hkv, Nk, D] views, packed [Hkv, Tk, D], or pages [num_pages, Hkv, page_size, D]
+    with block_table and max_seqlen_k, as the attention calls take it; the call's tokens are the newest of seq_lens (int32 [B];
+    None: Nk) or of cu_seqlens_k, their own rows included.  Returns (q_out, k_out, v_out); v_out is None without v.
+    """
+    tc = torch or _torch()
+    packed, paged = cu_seqlens_q is not None, block_table is not None
+    nd = 3 if packed else 4
+    _elements(tc, q, "q", dims=nd)
+    _elements(tc, k, "k", q, dims=nd)
+    if k.shape[-2] != q.shape[-2] or (not packed and k.shape[0] != q.shape[0]):
+        raise ValueError("q and k must have the same rows")
+    if v is not None:
+        _elements(tc, v, "v", q, dims=nd)
+        if v.shape != k.shape:
+            raise ValueError("v must be shaped like k")
+        if k_out is None or v_out is None:
+            raise ValueError("values are copied into a cache: k_out and v_out must be given")
+    elif v_out is not None:
+        raise ValueError("v_out without v")
+    if k_out is None:
+        if paged or seq_lens is not None or cu_seqlens_k is not None:
+            raise ValueError("a cache's lengths or pages without the cache: k_out must be given")
+        cu_seqlens_k, max_seqlen_k = cu_seqlens_q, max_seqlen_q
+        rows_of_cache = q.shape[-2]
+    else:
+        out_dims = 4 if paged else nd
+        _elements(tc, k_out, "k_out", q, k.shape[-3], out_dims)
+        if v is not None:
+            _elements(tc, v_out, "v_out", q, k.shape[-3], out_dims)
+            if v_out.shape != k_out.shape:
+                raise ValueError("k_out and v_out must have the same shape")
+        if not packed and not paged and k_out.shape[0] != q.shape[0]:
+            raise ValueError("k_out must have q's batch entries")
+        if packed and not paged and cu_seqlens_k is None:
+            cu_seqlens_k, max_seqlen_k = cu_seqlens_q, max_seqlen_q
+        rows_of_cache = k_out.shape[-2]
+    if q_out is not None:
+        _elements(tc, q_out, "q_out", q, dims=nd)
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must be shaped like q")
+    a = SwaaNormRopeArgs()
+    _fill_norm_rope(tc, a, q, k, inv_freq, q_weight, k_weight, eps, interleaved)
+    _fill_sequences(tc, a, q, rows_of_cache, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k, seq_lens, paged)
+    if paged:
+        _fill_pages(tc, a, k_out, block_table, a.B)
+    a.positions = _numbers(tc, positions, "positions", tc.int32, (q.shape[1],) if packed else (a.B, a.Nq), q)
+    a.total_rows_q = 0 if not packed else q.shape[1] if total_rows_q is None else int(total_rows_q)
+    a.q, a.k = _rows(q), _rows(k)
+    caller = None if stream is None else _stream_handle(None, q)
+    with _on_device_of(q) if stream is None else _launching_on(stream, q):
+        made = []
+        if q_out is None:
+            q_out = tc.empty(q.shape, dtype=q.dtype, device=q.device)
+            made.append(q_out)
+        if k_out is None:
+            k_out = tc.empty(k.shape, dtype=k.dtype, device=k.device)
+            made.append(k_out)
+        a.q_out, a.k_out = _rows(q_out), _rows(k_out)
+        if v is not None:
+            a.v, a.v_out = _rows(v), _rows(v_out)
+        a.stream = _stream_handle(stream, q)
+        _call("swaa_qk_norm_rope", a)
+        if stream is not None and made:
+            _returned_to(caller, *made)
+    return q_out, k_out, v_out
+
+
+def swaa_qk_norm_rope_bwd(dq_out, dk_out, q, k, inv_freq=None, positions=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                          interleaved: bool = False, dq=None, dk=None, workspace=None, stream=None):
+    """Gradients (dq, dk, dq_weight, dk_weight) of swaa_qk_norm_rope without a cache, from those of its results.
+
+    q, k, dq_out and dk_out as there, [B, H, N, D] views of one type; the other arguments as in the forward call.  dq and dk are
+    by default new tensors in q's and k's memory order; the weights' gradients are fp32 [D], None without weights.
+    workspace: a uint8 tensor of swaa_qk_norm_rope_bwd_workspace_bytes(...) bytes (allocated here with torch when None).
+    """
+    tc = torch or _torch()
+    _elements(tc, q, "q")
+    _elements(tc, k, "k", q)
+    for name, t, like in (("dq_out", dq_out, q), ("dk_out", dk_out, k), ("dq", dq, q), ("dk", dk, k)):
+        if t is not None:
+            _elements(tc, t, name, like)
+            if t.shape != like.shape:
+                raise ValueError(f"{name} must be shaped like {'q' if like is q else 'k'}")
+    if k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
+        raise ValueError("q and k must have the same rows")
+    a = SwaaNormRopeBwdArgs()
+    _fill_norm_rope(tc, a, q, k, inv_freq, q_weight, k_weight, eps, interleaved)
+    a.B, a.N = q.shape[0], q.shape[2]
+    a.positions = _numbers(tc, positions, "positions", tc.int32, (a.B, a.N), q)
+    a.q, a.k, a.dq_out, a.dk_out = _rows(q), _rows(k), _rows(dq_out), _rows(dk_out)
+    caller = None if stream is None else _stream_handle(None, q)
+    with _on_device_of(q) if stream is None else _launching_on(stream, q):
+        made = []
+        if dq is None:
+            dq = tc.empty_like(q)
+            made.append(dq)
+        if dk is None:
+            dk = tc.empty_like(k)
+            made.append(dk)
+        dq_weight = dk_weight = None
+        if q_weight is not None:
+            dq_weight, dk_weight = tc.empty_like(q_weight), tc.empty_like(k_weight)
+            made += [dq_weight, dk_weight]
+            a.dq_weight, a.dk_weight = dq_weight.data_ptr(), dk_weight.data_ptr()
+        a.dq, a.dk = _rows(dq), _rows(dk)
+        workspace = _scratch(tc, "swaa_qk_norm_rope_bwd", a, workspace, q.device)
+        a.stream = _stream_handle(stream, q)
+        _call("swaa_qk_norm_rope_bwd", a)
+        if stream is not None and made:
+            _returned_to(caller, *made)
+    return dq, dk, dq_weight, dk_weight
+
+
+def swaa_qk_norm_rope_bwd_workspace_bytes(B, Hq, Hkv, N, D) -> int:
+    """Bytes of device scratch swaa_qk_norm_rope_bwd needs with weights (without: none)."""
+    a = SwaaNormRopeBwdArgs()
+    a.B, a.Hq, a.Hkv, a.N, a.D, a.q_weight = int(B), int(Hq), int(Hkv), int(N), int(D), 4096  # (looked at for being there)
+    r = int(load_library().swaa_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(a)))
+    if r < 0:
+        raise SwaaError(r, swaa_status_string(r))
+    return r
+
+
+def swaa_attn_key_weights_workspace_bytes(B, Hq, Hkv, Nq, Nk, D) -> int:
+    """Bytes of device scratch swaa_attn_key_weights needs for this shape (often 0)."""
+    a = SwaaKeyWeightsArgs()
+    a.B, a.Hq, a.Hkv, a.Nq, a.Nk, a.D = int(B), int(Hq), int(Hkv), int(Nq), int(Nk), int(D)
+    r = int(load_library().swaa_attn_key_weights_workspace_bytes(ctypes.byref(a)))
+    if r < 0:
+        raise SwaaError(r, swaa_status_string(r))
+    return r
+
+
+def _fill_weights(tc, a, weights, B, Hkv, Nk, like):
+    if weights.dtype is not tc.float32 or weights.dim() != 3 or weights.get_device() != like.get_device() \
+            or weights.shape[0] != B or weights.shape[1] != Hkv or weights.shape[2] < Nk \
+            or (weights.shape[2] > 1 and weights.stride(2) != 1):
+        raise ValueError(f"weights must be an fp32 [{B}, {Hkv}, >= {Nk}] tensor with contiguous rows on the GPU of the others")
+    a.weights = weights.data_ptr()
+    a.weights_stride_b, a.weights_stride_h = (weights.stride(0) if B > 1 else 0), (weights.stride(1) if Hkv > 1 else 0)
+
+
+def swaa_attn_key_weights(q, k, lse, window: int, n_sink: int, n_prompt: int | None = None, scale: float | None = None,
+                          weights=None, decay: float = 0.0, cu_seqlens_q=None, cu_seqlens_k=None, max_seqlen_q: int | None = None,
+                          max_seqlen_k: int | None = None, seq_lens=None, block_table=None, n_prompts=None, workspace=None,
+                          stream=None):
+    """The attention weight each key has got from the rows of an attention call: decay * weights + its sum over those rows and the
+    query heads of its KV head, in place; what swaa_cache_evict judges keys by.
+
+    q, k, lse and the mask are those of the attention call (swaa_attn_fwd, _fwd_ex, _decode, _decode_ex; lse as it returned it):
+    q [B, Hq, Nq, D] or packed [Hq, Tq, D], k [B, Hkv, Nk, D], packed [Hkv, Tk, D], or pages with block_table; any head
+    dimension of swaa_attn_fwd.  weights: fp32 [B, Hkv, >= Nk] with contiguous rows, also for packed batches; entries behind a
+    sequence's length are left as they are.  None (only with decay 0): a new tensor, 0 there.  workspace: a uint8 tensor of
+    swaa_attn_key_weights_workspace_bytes(...) bytes (allocated here with torch when None).  Returns weights.
+    """
+    tc = torch or _torch()
+    packed, paged = cu_seqlens_q is not None, block_table is not None
+    _elements(tc, q, "q", dims=3 if packed else 4)
+    _elements(tc, k, "k", q, dims=3 if packed and not paged else 4)
+    if not packed and not paged and k.shape[0] != q.shape[0]:
+        raise ValueError("k must have q's batch entries")
+    a = SwaaKeyWeightsArgs()
+    a.Hq, a.Hkv, a.D = q.shape[-3], k.shape[-3], q.shape[-1]
+    _fill_sequences(tc, a, q, k.shape[-2], cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k, seq_lens, paged)
+    if paged:
+        _fill_pages(tc, a, k, block_table, a.B)
+    lse_shape = tuple(q.shape[:-1])
+    a.lse = _numbers(tc, lse, "lse", tc.float32, lse_shape, q)
+    a.lse_stride_b, a.lse_stride_h = (0, lse.stride(0)) if packed else (lse.stride(0), lse.stride(1))
+    a.n_prompts = _numbers(tc, n_prompts, "n_prompts", tc.int32, (a.B,), q)
+    a.window, a.n_sink = int(window), int(n_sink)
+    a.n_prompt = 2**31 - 1 if n_prompt is None else int(n_prompt)
+    a.scale, a.decay = 1.0 / math.sqrt(a.D) if scale is None else float(scale), float(decay)
+    a.dtype = SWAA_F16 if q.dtype is tc.float16 else SWAA_BF16
+    a.q, a.k = _rows(q), _rows(k)
+    caller = None if stream is None else _stream_handle(None, q)
+    with _on_device_of(q) if stream is None else _launching_on(stream, q):
+        made = weights is None
+        if made:
+            if decay != 0:
+                raise ValueError("decay without weights")
+            new = tc.zeros if packed or seq_lens is not None else tc.empty
+            weights = new((max(a.B, 0), a.Hkv, max(a.Nk, 0)), dtype=tc.float32, device=q.device)
+        _fill_weights(tc, a, weights, a.B, a.Hkv, a.Nk, q)
+        workspace = _scratch(tc, "swaa_attn_key_weights", a, workspace, q.device)
+        a.stream = _stream_handle(stream, q)
+        _call("swaa_attn_key_weights", a)
+        if stream is not None and made:
+            _returned_to(caller, weights)
+    return weights
+
+
+def swaa_cache_evict(k, v, weights, n_keep: int, n_sink: int, n_recent: int, seq_lens=None, block_table=None,
+                     max_seqlen_k: int | None = None, kept=None, new_lens=None, stream=None):
+    """Cuts every sequence of a cache that is longer than n_keep tokens to n_keep rows, per KV head: the first n_sink, the last
+    n_recent and the heaviest others by `weights` (swaa_attn_key_weights); they close up in place, weights with them.
+
+    k, v: bf16 or fp16 cache views [B, Hkv, Nk, D], or pages [num_pages, Hkv, page_size, D] with block_table (pages that no two
+    sequences share) and max_seqlen_k; weights fp32 [B, Hkv, >= Nk] with contiguous rows; seq_lens int32 [B] or None (Nk each).
+    All three are changed in place.  Returns (kept int32 [B, Hkv, n_keep], the rows that stayed, -1 behind shorter sequences',
+    new_lens int32 [B], the sequences' new lengths; new_lens=seq_lens updates those in place).
+    """
+    tc = torch or _torch()
+    paged = block_table is not None
+    _elements(tc, k, "k")
+    _elements(tc, v, "v", k, k.shape[1])
+    if v.shape != k.shape:
+        raise ValueError("k and v must have the same shape")
+    if paged and max_seqlen_k is None:
+        raise ValueError("a paged cache needs max_seqlen_k")
+    a = SwaaEvictArgs()
+    a.B, a.Hkv, a.D = block_table.shape[0] if paged else k.shape[0], k.shape[1], k.shape[3]
+    a.Nk = k.shape[2] if max_seqlen_k is None else int(max_seqlen_k)
+    if not paged and a.Nk > k.shape[2]:
+        raise ValueError("max_seqlen_k is more than the cache has rows")
+    if paged:
+        _fill_pages(tc, a, k, block_table, a.B)
+    a.seq_lens = _numbers(tc, seq_lens, "seq_lens", tc.int32, (a.B,), k)
+    _fill_weights(tc, a, weights, a.B, a.Hkv, a.Nk, k)
+    a.n_keep, a.n_sink, a.n_recent = int(n_keep), int(n_sink), int(n_recent)
+    a.k, a.v = _rows(k), _rows(v)
+    caller = None if stream is None else _stream_handle(None, k)
+    with _on_device_of(k) if stream is None else _launching_on(stream, k):
+        made = []
+        if kept is None:
+            kept = tc.empty((a.B, a.Hkv, max(a.n_keep, 0)), dtype=tc.int32, device=k.device)
+            made.append(kept)
+        if new_lens is None:
+            new_lens = tc.empty(a.B, dtype=tc.int32, device=k.device)
+            made.append(new_lens)
+        a.kept = _numbers(tc, kept, "kept", tc.int32, (a.B, a.Hkv, max(a.n_keep, 0)), k)
+        a.new_lens = _numbers(tc, new_lens, "new_lens", tc.int32, (a.B,), k)
+        a.stream = _stream_handle(stream, k)
+        _call("swaa_cache_evict", a)
+        if stream is not None and made:
+            _returned_to(caller, *made)
+    return kept, new_lens

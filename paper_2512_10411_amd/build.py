@@ -13,7 +13,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 SOURCES = [os.path.join(CSRC, f) for f in ("swaa_api.hip", "swaa_fwd_simple.hip", "swaa_fwd_d64.hip", "swaa_fwd_pipelined.hip",
                                             "swaa_fwd_short.hip",
-                                            "swaa_decode.hip", "swaa_bwd.hip", "swaa_bwd_dq_pipelined.hip")]
+                                            "swaa_decode.hip", "swaa_bwd.hip", "swaa_bwd_dq_pipelined.hip",
+                                            "swaa_norm_rope.hip", "swaa_key_weights.hip", "swaa_evict.hip")]
 LIB = os.path.join(PKG, "libswaa.so")
 
 HIPCC_FLAGS = [

@@ -6,6 +6,7 @@
 #include "swaa.h"
 #include "swaa_common.h"
 #include "swaa_bwd.h"
+#include "swaa_cache_ops.h"
 #include "swaa_decode.h"
 #include "swaa_fwd_short.h"
 
@@ -414,6 +415,259 @@ int swaa_attn_bwd(const void *q, const void *k, const void *v, const void *out, 
     p.partial = p.delta + (((long long)B * Hq * N + 3) / 4) * 4;
     const hipError_t err = swaa::launch_bwd(p, D, static_cast<hipStream_t>(stream));
     return err == hipSuccess ? SWAA_OK : SWAA_ERR_LAUNCH;
+}
+
+
+namespace {
+
+bool is_finite(float x) {
+    uint32_t u;
+    std::memcpy(&u, &x, sizeof u);
+    return ((u >> 23) & 0xffu) != 0xffu;
+}
+bool misaligned_words(const void *ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 3u) != 0; }
+
+// A tensor of `heads` heads whose batch stride may be 0 if it has one block (or its blocks are not its batch entries).
+int check_rows(const swaa_tensor &t, int heads, int D, bool one_block) {
+    if (misaligned(t.ptr)) return SWAA_ERR_ALIGN;
+    if (bad_stride(t.stride_n, false) || t.stride_n < D || t.stride_n >= (1LL << 22)) return SWAA_ERR_SHAPE;
+    if (bad_stride(t.stride_h, heads == 1) || bad_stride(t.stride_b, one_block)) return SWAA_ERR_SHAPE;
+    return SWAA_OK;
+}
+swaa::Rows rows_of(const swaa_tensor &t) { return {static_cast<char *>(t.ptr), t.stride_b, t.stride_h, t.stride_n}; }
+
+int check_heads(int B, int Hq, int Hkv, int D) {
+    if (B < 1 || Hq < 1 || Hkv < 1 || D < 1 || Hq % Hkv != 0) return SWAA_ERR_SHAPE;
+    return D % 32 != 0 || D > 256 ? SWAA_ERR_UNSUPPORTED : SWAA_OK;
+}
+
+// The sequences of a call of the cache's operators.
+int set_sequences(swaa::Sequences &s, int B, int Nq, int Nk, const int *cu_q, const int *cu_k, const int *seq_lens) {
+    if (Nq < 1 || Nk < 1) return SWAA_ERR_SHAPE;
+    const bool packed = cu_q || cu_k;
+    if (packed && (!cu_q || !cu_k)) return SWAA_ERR_NULL;
+    if (packed && seq_lens) return SWAA_ERR_SHAPE;  // (packed sequences have their lengths from the offsets)
+    if (!packed && Nq > Nk) return SWAA_ERR_SHAPE;  // the rows are the newest Nq of Nk tokens
+    if (misaligned_words(cu_q) || misaligned_words(cu_k) || misaligned_words(seq_lens)) return SWAA_ERR_ALIGN;
+    s = {cu_q, cu_k, seq_lens, B, Nq, Nk};
+    return SWAA_OK;
+}
+
+int set_pages(swaa::Pages &p, const int *table, int table_stride, int page_size, int num_pages, int Nk) {
+    p = {nullptr, 0, 1, 1, swaa::make_fastdiv(1)};
+    if (!table) return SWAA_OK;
+    if (page_size < 1 || num_pages < 1 || table_stride < 1) return SWAA_ERR_SHAPE;
+    if ((long long)table_stride * page_size < Nk) return SWAA_ERR_SHAPE;  // table too short for Nk tokens
+    if (misaligned_words(table)) return SWAA_ERR_ALIGN;
+    p = {table, table_stride, page_size, num_pages, swaa::make_fastdiv((unsigned)page_size)};
+    return SWAA_OK;
+}
+
+// Norms and rotation: what forward and backward have in common.
+int set_norm_rope(swaa::NormRopeParams &p, int Hq, int Hkv, int D, const int *positions, const float *q_weight, const float *k_weight,
+                  float eps, const float *inv_freq, int rot_dim, int interleaved, int dtype) {
+    if (dtype != SWAA_BF16 && dtype != SWAA_F16) return SWAA_ERR_UNSUPPORTED;
+    if (!q_weight != !k_weight) return SWAA_ERR_NULL;
+    if (q_weight && !positive_finite(eps)) return SWAA_ERR_SHAPE;
+    if (rot_dim < 0 || rot_dim > D) return SWAA_ERR_SHAPE;
+    if (rot_dim % 16 != 0) return SWAA_ERR_UNSUPPORTED;
+    if (rot_dim > 0 && !inv_freq) return SWAA_ERR_NULL;
+    for (const void *ptr : {(const void *)positions, (const void *)q_weight, (const void *)k_weight, (const void *)inv_freq})
+        if (misaligned_words(ptr)) return SWAA_ERR_ALIGN;
+    p.positions = positions;
+    p.q_weight = q_weight;
+    p.k_weight = k_weight;
+    p.eps = eps;
+    p.inv_freq = inv_freq;
+    p.R = rot_dim;
+    p.interleaved = interleaved != 0;
+    p.fp16 = dtype == SWAA_F16 ? 1 : 0;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.D = D;
+    return SWAA_OK;
+}
+
+}  // namespace
+
+int swaa_qk_norm_rope(const swaa_norm_rope_args *a) {
+    if (!a) return SWAA_ERR_NULL;
+    if (!a->q.ptr || !a->k.ptr || !a->q_out.ptr || !a->k_out.ptr || (a->v.ptr && !a->v_out.ptr)) return SWAA_ERR_NULL;
+    int rc = check_heads(a->B, a->Hq, a->Hkv, a->D);
+    swaa::NormRopeParams p{};
+    if (rc == SWAA_OK) rc = set_sequences(p.seq, a->B, a->Nq, a->Nk, a->cu_seqlens_q, a->cu_seqlens_k, a->seq_lens);
+    if (rc == SWAA_OK) rc = set_pages(p.pages, a->block_table, a->block_table_stride, a->page_size, a->num_pages, a->Nk);
+    if (rc == SWAA_OK)
+        rc = set_norm_rope(p, a->Hq, a->Hkv, a->D, a->positions, a->q_weight, a->k_weight, a->eps, a->inv_freq, a->rot_dim, a->interleaved, a->dtype);
+    if (rc != SWAA_OK) return rc;
+    if (a->total_rows_q < 0) return SWAA_ERR_SHAPE;
+    const bool packed = a->cu_seqlens_q != nullptr, one = packed || a->B == 1, one_page = a->block_table ? a->num_pages == 1 : one;
+    if ((rc = check_rows(a->q, a->Hq, a->D, one)) != SWAA_OK || (rc = check_rows(a->k, a->Hkv, a->D, one)) != SWAA_OK ||
+        (rc = check_rows(a->q_out, a->Hq, a->D, one)) != SWAA_OK || (rc = check_rows(a->k_out, a->Hkv, a->D, one_page)) != SWAA_OK)
+        return rc;
+    if (a->v.ptr && ((rc = check_rows(a->v, a->Hkv, a->D, one)) != SWAA_OK || (rc = check_rows(a->v_out, a->Hkv, a->D, one_page)) != SWAA_OK))
+        return rc;
+    p.q = rows_of(a->q);
+    p.k = rows_of(a->k);
+    p.q_out = rows_of(a->q_out);
+    p.k_out = rows_of(a->k_out);
+    if (a->v.ptr) {
+        p.v = rows_of(a->v);
+        p.v_out = rows_of(a->v_out);
+    }
+    p.by_row = packed && a->total_rows_q > 0;
+    p.tokens = p.by_row ? a->total_rows_q : (long long)a->B * a->Nq;
+    p.div_nq = swaa::make_fastdiv((unsigned)a->Nq);
+    if (p.tokens > 0x7fffffffLL || !swaa::plan_norm_rope(p)) return SWAA_ERR_SHAPE;
+    return swaa::launch_norm_rope(p, static_cast<hipStream_t>(a->stream)) == hipSuccess ? SWAA_OK : SWAA_ERR_LAUNCH;
+}
+
+namespace {
+
+int norm_rope_bwd_plan(const swaa_norm_rope_bwd_args *a, swaa::NormRopeParams &p, long long &ws_bytes) {
+    int rc = check_heads(a->B, a->Hq, a->Hkv, a->D);
+    if (rc == SWAA_OK) rc = set_sequences(p.seq, a->B, a->N, a->N, nullptr, nullptr, nullptr);
+    if (rc != SWAA_OK) return rc;
+    p.Hq = a->Hq;
+    p.Hkv = a->Hkv;
+    p.D = a->D;
+    p.tokens = (long long)a->B * a->N;
+    p.div_nq = swaa::make_fastdiv((unsigned)a->N);
+    if (p.tokens > 0x7fffffffLL || !swaa::plan_norm_rope_bwd(p)) return SWAA_ERR_SHAPE;
+    ws_bytes = a->q_weight ? p.wgs * 2 * a->D * (long long)sizeof(float) : 0;
+    return SWAA_OK;
+}
+
+}  // namespace
+
+long long swaa_qk_norm_rope_bwd_workspace_bytes(const swaa_norm_rope_bwd_args *a) {
+    if (!a) return SWAA_ERR_NULL;
+    swaa::NormRopeParams p{};
+    long long bytes = 0;
+    const int rc = norm_rope_bwd_plan(a, p, bytes);
+    return rc != SWAA_OK ? rc : bytes;
+}
+
+int swaa_qk_norm_rope_bwd(const swaa_norm_rope_bwd_args *a) {
+    if (!a) return SWAA_ERR_NULL;
+    if (!a->q.ptr || !a->k.ptr || !a->dq_out.ptr || !a->dk_out.ptr || !a->dq.ptr || !a->dk.ptr) return SWAA_ERR_NULL;
+    swaa::NormRopeParams p{};
+    long long need = 0;
+    int rc = norm_rope_bwd_plan(a, p, need);
+    if (rc == SWAA_OK)
+        rc = set_norm_rope(p, a->Hq, a->Hkv, a->D, a->positions, a->q_weight, a->k_weight, a->eps, a->inv_freq, a->rot_dim, a->interleaved, a->dtype);
+    if (rc != SWAA_OK) return rc;
+    if (a->q_weight && (!a->dq_weight || !a->dk_weight)) return SWAA_ERR_NULL;
+    for (const swaa_tensor *t : {&a->q, &a->dq_out, &a->dq, &a->k, &a->dk_out, &a->dk}) {
+        const bool of_q = t == &a->q || t == &a->dq_out || t == &a->dq;
+        if ((rc = check_rows(*t, of_q ? a->Hq : a->Hkv, a->D, a->B == 1)) != SWAA_OK) return rc;
+    }
+    if (misaligned_words(a->dq_weight) || misaligned_words(a->dk_weight)) return SWAA_ERR_ALIGN;
+    if (need > 0 && (!a->workspace || misaligned(a->workspace) || a->workspace_bytes < need)) return SWAA_ERR_WORKSPACE;
+    p.q = rows_of(a->q);
+    p.k = rows_of(a->k);
+    p.dq_out = rows_of(a->dq_out);
+    p.dk_out = rows_of(a->dk_out);
+    p.q_out = rows_of(a->dq);
+    p.k_out = rows_of(a->dk);
+    p.partial = need > 0 ? static_cast<float *>(a->workspace) : nullptr;
+    p.dq_weight = a->dq_weight;
+    p.dk_weight = a->dk_weight;
+    return swaa::launch_norm_rope_bwd(p, static_cast<hipStream_t>(a->stream)) == hipSuccess ? SWAA_OK : SWAA_ERR_LAUNCH;
+}
+
+namespace {
+
+int key_weights_plan(const swaa_key_weights_args *a, swaa::KeyWeightsParams &p) {
+    int rc = check_heads(a->B, a->Hq, a->Hkv, a->D);
+    if (rc == SWAA_OK) rc = set_sequences(p.seq, a->B, a->Nq, a->Nk, a->cu_seqlens_q, a->cu_seqlens_k, a->seq_lens);
+    if (rc != SWAA_OK) return rc;
+    p.Hq = a->Hq;
+    p.G = a->Hq / a->Hkv;
+    p.D = a->D;
+    return (long long)a->B * a->Hkv <= 0x7fffffffLL && swaa::plan_key_weights(p) ? SWAA_OK : SWAA_ERR_SHAPE;
+}
+
+}  // namespace
+
+long long swaa_attn_key_weights_workspace_bytes(const swaa_key_weights_args *a) {
+    if (!a) return SWAA_ERR_NULL;
+    swaa::KeyWeightsParams p{};
+    const int rc = key_weights_plan(a, p);
+    return rc != SWAA_OK ? rc : swaa::key_weights_workspace_bytes(p);
+}
+
+int swaa_attn_key_weights(const swaa_key_weights_args *a) {
+    if (!a) return SWAA_ERR_NULL;
+    if (!a->q.ptr || !a->k.ptr || !a->lse || !a->weights) return SWAA_ERR_NULL;
+    swaa::KeyWeightsParams p{};
+    int rc = key_weights_plan(a, p);
+    if (rc == SWAA_OK) rc = set_pages(p.pages, a->block_table, a->block_table_stride, a->page_size, a->num_pages, a->Nk);
+    if (rc != SWAA_OK) return rc;
+    if (a->window < 1 || a->n_sink < 0 || a->n_prompt < 0) return SWAA_ERR_SHAPE;
+    if (!positive_finite(a->scale) || !is_finite(a->decay) || a->decay < 0.f) return SWAA_ERR_SHAPE;
+    if (a->dtype != SWAA_BF16 && a->dtype != SWAA_F16) return SWAA_ERR_UNSUPPORTED;
+    const bool one = a->cu_seqlens_q || a->B == 1;
+    if ((rc = check_rows(a->q, a->Hq, a->D, one)) != SWAA_OK ||
+        (rc = check_rows(a->k, a->Hkv, a->D, a->block_table ? a->num_pages == 1 : one)) != SWAA_OK)
+        return rc;
+    if (misaligned_words(a->lse) || misaligned_words(a->weights) || misaligned_words(a->n_prompts)) return SWAA_ERR_ALIGN;
+    if (a->lse_stride_b < 0 || a->lse_stride_h < 0) return SWAA_ERR_SHAPE;
+    // (two keys must not share a weight)
+    if ((a->Hkv > 1 && a->weights_stride_h < a->Nk) || (a->B > 1 && a->weights_stride_b < a->Nk)) return SWAA_ERR_SHAPE;
+    const long long need = swaa::key_weights_workspace_bytes(p);
+    if (need > 0 && (!a->workspace || misaligned(a->workspace) || a->workspace_bytes < need)) return SWAA_ERR_WORKSPACE;
+    p.q = rows_of(a->q);
+    p.k = rows_of(a->k);
+    p.lse = a->lse;
+    p.lse_sb = a->lse_stride_b;
+    p.lse_sh = a->lse_stride_h;
+    p.weights = a->weights;
+    p.w_sb = a->weights_stride_b;
+    p.w_sh = a->weights_stride_h;
+    p.n_prompts = a->n_prompts;
+    p.fp16 = a->dtype == SWAA_F16 ? 1 : 0;
+    p.W = a->window < a->Nk ? a->window : a->Nk;
+    p.S = a->n_sink < a->Nk ? a->n_sink : a->Nk;
+    p.P = a->n_prompt < a->Nk ? a->n_prompt : a->Nk;
+    p.scale_log2 = a->scale * 1.44269504088896340736f;
+    p.decay = a->decay;
+    p.partial = static_cast<float *>(a->workspace);
+    return swaa::launch_key_weights(p, static_cast<hipStream_t>(a->stream)) == hipSuccess ? SWAA_OK : SWAA_ERR_LAUNCH;
+}
+
+int swaa_cache_evict(const swaa_evict_args *a) {
+    if (!a) return SWAA_ERR_NULL;
+    if (!a->k.ptr || !a->v.ptr || !a->weights || !a->kept) return SWAA_ERR_NULL;
+    int rc = check_heads(a->B, a->Hkv, a->Hkv, a->D);
+    swaa::EvictParams p{};
+    if (rc == SWAA_OK && a->Nk < 1) rc = SWAA_ERR_SHAPE;
+    if (rc == SWAA_OK) rc = set_pages(p.pages, a->block_table, a->block_table_stride, a->page_size, a->num_pages, a->Nk);
+    if (rc != SWAA_OK) return rc;
+    if (a->n_keep < 1 || a->n_sink < 0 || a->n_recent < 0 || (long long)a->n_sink + a->n_recent > a->n_keep) return SWAA_ERR_SHAPE;
+    const bool one = a->block_table ? a->num_pages == 1 : a->B == 1;
+    if ((rc = check_rows(a->k, a->Hkv, a->D, one)) != SWAA_OK || (rc = check_rows(a->v, a->Hkv, a->D, one)) != SWAA_OK) return rc;
+    for (const void *ptr : {(const void *)a->weights, (const void *)a->kept, (const void *)a->new_lens, (const void *)a->seq_lens})
+        if (misaligned_words(ptr)) return SWAA_ERR_ALIGN;
+    if ((a->Hkv > 1 && a->weights_stride_h < a->Nk) || (a->B > 1 && a->weights_stride_b < a->Nk)) return SWAA_ERR_SHAPE;
+    if ((long long)a->B * a->Hkv > 0x7fffffffLL / 256) return SWAA_ERR_SHAPE;
+    p.k = rows_of(a->k);
+    p.v = rows_of(a->v);
+    p.weights = a->weights;
+    p.w_sb = a->weights_stride_b;
+    p.w_sh = a->weights_stride_h;
+    p.kept = a->kept;
+    p.new_lens = a->new_lens;
+    p.seq_lens = a->seq_lens;
+    p.B = a->B;
+    p.Hkv = a->Hkv;
+    p.D = a->D;
+    p.Nk = a->Nk;
+    p.n_keep = a->n_keep;
+    p.n_sink = a->n_sink;
+    p.n_recent = a->n_recent;
+    p.div_hkv = swaa::make_fastdiv((unsigned)a->Hkv);
+    return swaa::launch_evict(p, static_cast<hipStream_t>(a->stream)) == hipSuccess ? SWAA_OK : SWAA_ERR_LAUNCH;
 }
 
 }  // extern "C"

@@ -1,0 +1,119 @@
+"""swaa_cache_evict against its definition: which rows stay, and that exactly their bits are where they belong."""
+import math
+
+import pytest
+import torch
+
+import cache_ops_ref as ref
+from paper_2512_10411_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+
+def run(kind, lens, H, D, n_keep, n_sink, n_recent, weights, gen, page_size=16, dtype=torch.bfloat16, Nk=None, **kw):
+    B, Nk = len(lens), Nk or max(lens)
+    kc, vc = (ref.Cache(kind, B, H, Nk, D, dtype, torch.Generator().manual_seed(s), page_size) for s in (1, 2))
+    if kind == "paged":
+        vc.host_table, vc.table = kc.host_table, kc.table
+    w = weights.cuda()
+    seq = torch.tensor(lens, dtype=torch.int32).cuda()
+    kept, new = binding.swaa_cache_evict(kc.view, vc.view, w, n_keep, n_sink, n_recent, seq_lens=seq, block_table=kc.table,
+                                         max_seqlen_k=Nk, **kw)
+    torch.cuda.synchronize()
+    assert new.tolist() == [min(n, n_keep) for n in lens]
+    kept, got_w = kept.cpu(), w.cpu()
+    for b, n in enumerate(lens):
+        left = min(n, n_keep)
+        for g in range(H):
+            want = ref.evict(weights[b, g, :n], n, n_keep, n_sink, n_recent)
+            assert kept[b, g].tolist() == want + [-1] * (n_keep - left), (b, g)
+            rows = torch.tensor(want, dtype=torch.long)
+            expect = weights[b, g].clone()
+            expect[:left] = weights[b, g, rows]
+            expect[left:n] = 0
+            assert torch.equal(got_w[b, g].view(torch.int32), expect.view(torch.int32))
+            for c in (kc, vc):
+                assert torch.equal(c.rows(b, left, c.gpu.cpu())[g].view(torch.int16), c.rows(b, n)[g, rows].view(torch.int16)), (b, g)
+    return kc, vc, kept
+
+
+def random_weights(B, H, N, gen, ties=0):
+    w = (2 * torch.randn(B, H, N, generator=gen)).exp()
+    return w if not ties else torch.randint(0, ties, w.shape, generator=gen).float()
+
+
+# lens, H, D, n_keep, n_sink, n_recent
+SHAPES = [([1], 1, 128, 1, 0, 0), ([5], 1, 64, 4, 1, 1), ([100, 40, 64, 65], 2, 128, 64, 4, 10), ([900], 2, 128, 300, 0, 0),
+          ([300, 301], 3, 32, 300, 100, 200), ([777], 1, 96, 500, 499, 0), ([777], 1, 256, 500, 0, 499), ([4097, 0, 1], 2, 64, 1000, 3, 50),
+          ([50], 1, 160, 100, 4, 10), ([5000, 4096], 1, 224, 4095, 4, 1), ([64], 2, 192, 1, 0, 1)]
+
+
+@pytest.mark.parametrize("ties", [0, 3, 1])
+@pytest.mark.parametrize("kind", ["dense", "rows", "paged"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_which_rows_stay_and_where(shape, kind, ties):
+    lens, H, D, n_keep, n_sink, n_recent = shape
+    print(f"[case] {shape} {kind} ties {ties}", flush=True)
+    gen = torch.Generator().manual_seed(sum(lens) + ties)
+    run(kind, lens, H, D, n_keep, n_sink, n_recent, random_weights(len(lens), H, max(lens) + 3, gen, ties), gen)
+
+
+@pytest.mark.parametrize("page_size", [1, 3, 64])
+def test_pages_of_any_size(page_size):
+    gen = torch.Generator().manual_seed(page_size)
+    run("paged", [333, 20, 150], 2, 128, 100, 4, 20, random_weights(3, 2, 333, gen), gen, page_size, torch.float16)
+
+
+@pytest.mark.parametrize("n", [32768, 32769, 70001, 140000])
+def test_long_sequences(n):
+    gen = torch.Generator().manual_seed(n)
+    run("dense", [n], 2, 32, n // 3, 7, 1000, random_weights(1, 2, n, gen, ties=0 if n % 2 else 50), gen)
+
+
+def test_weights_that_are_no_ordinary_numbers():
+    gen = torch.Generator().manual_seed(7)
+    w = torch.randn(1, 2, 200, generator=gen)  # (negative ones among them)
+    w[0, 0, 10], w[0, 0, 50], w[0, 0, 51] = float("nan"), math.inf, -math.inf
+    w[0, 0, 60:90] = 0.0
+    w[0, 0, 70:80] = -0.0
+    w[0, 1] = float("nan")
+    w[0, 1, 100:] = -math.inf
+    for n_keep in (1, 20, 110, 150, 199):
+        run("dense", [200], 2, 64, n_keep, 0, 0, w, gen)
+
+
+def test_lengths_without_an_array_and_in_place():
+    gen = torch.Generator().manual_seed(5)
+    k, v = (torch.randn(2, 2, 300, 64, generator=gen).half().cuda() for _ in range(2))
+    w = random_weights(2, 2, 300, gen).cuda()
+    first = [t.clone() for t in (k, v, w)]
+    kept, new = binding.swaa_cache_evict(k, v, w, 100, 4, 20)
+    assert new.tolist() == [100, 100]
+    for t, was in ((k, first[0]), (v, first[1])):
+        assert torch.equal(t[:, :, :100], was.gather(2, kept.long()[..., None].expand(-1, -1, -1, 64)))
+    # lengths updated in place, results in tensors of the caller's
+    k2, v2, w2 = (t.clone() for t in first)
+    lens, mine = torch.tensor([300, 300], dtype=torch.int32).cuda(), torch.zeros_like(kept)
+    got = binding.swaa_cache_evict(k2, v2, w2, 100, 4, 20, seq_lens=lens, kept=mine, new_lens=lens)
+    assert got[0] is mine and got[1] is lens and lens.tolist() == [100, 100]
+    assert torch.equal(mine, kept) and torch.equal(k2[:, :, :100], k[:, :, :100]) and torch.equal(w2, w)
+
+
+def test_pages_outside_the_cache():
+    """They are read clamped and not written; other sequences' rows are their own."""
+    gen = torch.Generator().manual_seed(3)
+    kc, vc = (ref.Cache("paged", 2, 1, 96, 64, torch.bfloat16, torch.Generator().manual_seed(s)) for s in (1, 2))
+    vc.host_table = kc.host_table
+    pages = kc.data.shape[0]
+    good = kc.host_table.clone()
+    kc.host_table[0, 0], kc.host_table[0, 3] = pages + 7, -5
+    w = random_weights(2, 1, 96, gen)
+    binding.swaa_cache_evict(kc.view, vc.view, w.cuda(), 40, 0, 0, seq_lens=torch.tensor([96, 90], dtype=torch.int32).cuda(),
+                             block_table=kc.host_table.cuda(), max_seqlen_k=96)
+    rows = torch.tensor(ref.evict(w[1, 0, :90], 90, 40, 0, 0))
+    for c in (kc, vc):
+        data = c.gpu.cpu()
+        assert torch.equal(c.rows(1, 40, data), c.rows(1, 90)[:, rows])
+        named = set(good.flatten().tolist())
+        strangers = [p for p in range(pages) if p not in named] + [int(good[0, 0]), int(good[0, 3])]  # (in no table now)
+        assert torch.equal(data[strangers], c.data[strangers])
