@@ -526,7 +526,8 @@ typedef struct swaa_key_weights_args {
 
 int swaa_attn_key_weights(const swaa_key_weights_args *args);
 
-/* Bytes of workspace swaa_attn_key_weights needs: reads the shape fields (B, Hq, Hkv, D, Nq, Nk).  Host-only arithmetic. */
+/* Bytes of workspace swaa_attn_key_weights needs: reads the fields of shape and mask and whether n_prompts is NULL; below 16 MiB.
+ * Host-only arithmetic. */
 long long swaa_attn_key_weights_workspace_bytes(const swaa_key_weights_args *args);
 
 /*

@@ -1053,9 +1053,12 @@ def swaa_qk_norm_rope_bwd_workspace_bytes(B, Hq, Hkv, N, D) -> int:
     return r
 
 
-def swaa_attn_key_weights_workspace_bytes(B, Hq, Hkv, Nq, Nk, D) -> int:
-    """Bytes of device scratch swaa_attn_key_weights needs for this shape (often 0)."""
+def swaa_attn_key_weights_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, window, n_sink, n_prompt=None, n_prompts=False) -> int:
+    """Bytes of device scratch swaa_attn_key_weights needs for this shape and mask (often 0); n_prompts: are there prompt lengths of
+    the sequences' own?"""
     a = SwaaKeyWeightsArgs()
+    a.window, a.n_sink, a.n_prompt = int(window), int(n_sink), 2**31 - 1 if n_prompt is None else int(n_prompt)
+    a.n_prompts = 4096 if n_prompts else None  # (looked at for being there)
     a.B, a.Hq, a.Hkv, a.Nq, a.Nk, a.D = int(B), int(Hq), int(Hkv), int(Nq), int(Nk), int(D)
     r = int(load_library().swaa_attn_key_weights_workspace_bytes(ctypes.byref(a)))
     if r < 0:

@@ -582,6 +582,11 @@ int key_weights_plan(const swaa_key_weights_args *a, swaa::KeyWeightsParams &p) 
     int rc = check_heads(a->B, a->Hq, a->Hkv, a->D);
     if (rc == SWAA_OK) rc = set_sequences(p.seq, a->B, a->Nq, a->Nk, a->cu_seqlens_q, a->cu_seqlens_k, a->seq_lens);
     if (rc != SWAA_OK) return rc;
+    if (a->window < 1 || a->n_sink < 0 || a->n_prompt < 0) return SWAA_ERR_SHAPE;
+    p.W = a->window < a->Nk ? a->window : a->Nk;
+    p.S = a->n_sink < a->Nk ? a->n_sink : a->Nk;
+    p.P = a->n_prompt < a->Nk ? a->n_prompt : a->Nk;
+    p.n_prompts = a->n_prompts;
     p.Hq = a->Hq;
     p.G = a->Hq / a->Hkv;
     p.D = a->D;
@@ -604,7 +609,6 @@ int swaa_attn_key_weights(const swaa_key_weights_args *a) {
     int rc = key_weights_plan(a, p);
     if (rc == SWAA_OK) rc = set_pages(p.pages, a->block_table, a->block_table_stride, a->page_size, a->num_pages, a->Nk);
     if (rc != SWAA_OK) return rc;
-    if (a->window < 1 || a->n_sink < 0 || a->n_prompt < 0) return SWAA_ERR_SHAPE;
     if (!positive_finite(a->scale) || !is_finite(a->decay) || a->decay < 0.f) return SWAA_ERR_SHAPE;
     if (a->dtype != SWAA_BF16 && a->dtype != SWAA_F16) return SWAA_ERR_UNSUPPORTED;
     const bool one = a->cu_seqlens_q || a->B == 1;
@@ -625,14 +629,10 @@ int swaa_attn_key_weights(const swaa_key_weights_args *a) {
     p.weights = a->weights;
     p.w_sb = a->weights_stride_b;
     p.w_sh = a->weights_stride_h;
-    p.n_prompts = a->n_prompts;
     p.fp16 = a->dtype == SWAA_F16 ? 1 : 0;
-    p.W = a->window < a->Nk ? a->window : a->Nk;
-    p.S = a->n_sink < a->Nk ? a->n_sink : a->Nk;
-    p.P = a->n_prompt < a->Nk ? a->n_prompt : a->Nk;
     p.scale_log2 = a->scale * 1.44269504088896340736f;
     p.decay = a->decay;
-    p.partial = static_cast<float *>(a->workspace);
+    p.partial = need > 0 ? static_cast<float *>(a->workspace) : nullptr;
     return swaa::launch_key_weights(p, static_cast<hipStream_t>(a->stream)) == hipSuccess ? SWAA_OK : SWAA_ERR_LAUNCH;
 }
 

@@ -93,11 +93,13 @@ struct KeyWeightsParams {
     int Hq, Hkv, G, D;
     int W, S, P;
     float scale_log2, decay;
-    // Work: (sequence, KV head) pairs x tiles of keys x chunks of the columns (heads of the group x rows that see the tile)
-    int pairs, tiles, chunks;
-    long long chunk_cols;
-    FastDiv div_pairs, div_tiles, div_hkv;
-    float *partial;  // [pairs][tiles][chunks][keys of a tile], chunks > 1 only
+    // Work (plan_key_weights): (sequence, KV head) pairs x (tiles of keys x chunks of the columns, heads of the group x rows that see
+    // the tile).  A row sees few keys of a windowed layer, but the sinks are seen by all: their tiles have chunk counts of their own.
+    int pairs, tiles, sink_tiles, sink_items;
+    int chunks, sink_chunks;
+    long long chunk_cols, items;
+    FastDiv div_pairs, div_hkv, div_sink_chunks, div_others;
+    float *partial;  // [items][keys of a tile], or null: one chunk per tile
 };
 constexpr int kKeyTile = 256;  // keys of a workgroup
 bool plan_key_weights(KeyWeightsParams &p);

@@ -87,17 +87,18 @@ def test_key_weights_refusals(status, kw):
 
 
 def test_key_weights_workspace():
-    a = dict(Nq=4000, Nk=4000, weights_stride_b=8000, weights_stride_h=4000, q=rows(4, 4000, 128), k=rows(2, 4000, 128))
-    need = binding.swaa_attn_key_weights_workspace_bytes(2, 4, 2, 4000, 4000, 128)
+    a = dict(Nq=4000, Nk=4000, window=4000, weights_stride_b=8000, weights_stride_h=4000, q=rows(4, 4000, 128), k=rows(2, 4000, 128))
+    need = binding.swaa_attn_key_weights_workspace_bytes(2, 4, 2, 4000, 4000, 128, 4000, 0)
     assert need > 0
     assert key_weights(workspace_bytes=need - 1, **a) == binding.SWAA_ERR_WORKSPACE
     assert key_weights(workspace=None, **a) == binding.SWAA_ERR_WORKSPACE
-    assert binding.swaa_attn_key_weights_workspace_bytes(1, 32, 8, 1, 131072, 128) == 0  # a new token: nothing to share out
+    assert binding.swaa_attn_key_weights_workspace_bytes(1, 32, 8, 1, 131072, 128, 131072, 4) == 0  # a new token: nothing to share out
     for shape in ((1, 32, 8, 131072, 131072, 128), (64, 40, 8, 2048, 131072, 128), (1, 8, 8, 1 << 20, 1 << 20, 64)):
-        assert binding.swaa_attn_key_weights_workspace_bytes(*shape) <= 1 << 30
+        for mask in ((1 << 30, 0), (8192, 4), (1, 0)):
+            assert binding.swaa_attn_key_weights_workspace_bytes(*shape, *mask) < 16 << 20
     for bad in ((1, 3, 2, 1, 1, 128), (1, 2, 2, 2, 1, 128), (0, 2, 2, 1, 1, 128), (1, 2, 2, 1, 1, 100)):
         with pytest.raises(binding.SwaaError):
-            binding.swaa_attn_key_weights_workspace_bytes(*bad)
+            binding.swaa_attn_key_weights_workspace_bytes(*bad, 10, 0)
 
 
 def test_norm_rope_bwd_workspace():

@@ -153,7 +153,7 @@ def test_the_same_bits_again_and_with_a_workspace_of_the_callers():
     gen = torch.Generator(device="cuda").manual_seed(41)
     q, k = torch.randn(1, 8, 3001, 128, generator=gen, device="cuda").bfloat16(), torch.randn(1, 2, 3001, 128, generator=gen, device="cuda").bfloat16()
     _, lse = binding.swaa_attn_fwd(q, torch.clone(k), k, 3001, 0)
-    need = binding.swaa_attn_key_weights_workspace_bytes(1, 8, 2, 3001, 3001, 128)
+    need = binding.swaa_attn_key_weights_workspace_bytes(1, 8, 2, 3001, 3001, 128, 3001, 0)
     assert need > 0
     first = binding.swaa_attn_key_weights(q, k, lse, 3001, 0)
     ws = torch.full((need,), 0xff, dtype=torch.uint8, device="cuda")
