@@ -96,8 +96,8 @@ struct KeyWeightsParams {
     // Work (plan_key_weights): (sequence, KV head) pairs x (tiles of keys x chunks of the columns, heads of the group x rows that see
     // the tile).  A row sees few keys of a windowed layer, but the sinks are seen by all: their tiles have chunk counts of their own.
     int pairs, tiles, sink_tiles, sink_items;
-    int chunks, sink_chunks;
-    long long chunk_cols, items;
+    int chunks, sink_chunks, chunk_stages;  // (stages of 64 columns)
+    long long items;
     FastDiv div_pairs, div_hkv, div_sink_chunks, div_others;
     float *partial;  // [items][keys of a tile], or null: one chunk per tile
 };

@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kWThreads = 256;
 constexpr int kMinChunk = 256;    // columns a workgroup goes through at least, if there are as many
-constexpr int kFillItems = 2048;  // workgroups that a call should have
+constexpr int kFillItems = 4096;  // workgroups that a call should have
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -69,25 +69,39 @@ __device__ __forceinline__ Item item_of(const KeyWeightsParams &p, unsigned id) 
     return w;
 }
 
-// What the keys of a tile are told about a column.
-struct Column {
-    float lse2;   // log2 units
-    int pos, lo;  // the row sees the keys up to pos that lie above lo, and the sinks; pos -1: nothing (no such column)
-    int pad;
+// The columns of a tile, kCols to a stage: head by head, each one's rows from the start of a stage on, or, where a head has few, all
+// heads' in a row.
+template <int kCols>
+struct Columns {
+    bool by_head;
+    int per_head, stages;
+    __host__ __device__ Columns(int n_all, int G) {
+        by_head = n_all >= 64;
+        per_head = (n_all + kCols - 1) / kCols;
+        stages = by_head ? G * per_head : (G * n_all + kCols - 1) / kCols;
+    }
 };
 
-// LDS: two buffers of kCols rows of Q without padding, then two of kCols Columns.  16-byte chunk c of row r lies at chunk
-// c ^ turn(r), so that eight rows' equal chunks lie in different banks; the copies apply it on the global side.
+// LDS: two buffers of kCols rows of Q without padding, then two of what the keys are told about each column: its lse in log2 units,
+// `pos` and `lo` (its row sees the keys up to pos that lie above lo, and the sinks; pos -1: nothing, no such column).  16-byte
+// chunk c of row r lies at chunk c ^ turn(r), so that the equal chunks of 16 rows lie in different banks (64 of 4 bytes); the copies
+// apply it on the global side.
+__host__ __device__ constexpr int stage_cols(int D) { return D <= 128 ? 64 : 32; }
 template <int D>
 struct Stage {
-    static constexpr int kCols = D <= 128 ? 64 : 32;
+    static constexpr int kCols = stage_cols(D);
     static constexpr int kRowB = D * 2, kBufB = kCols * kRowB;
-    static constexpr int kColumns = 2 * kBufB;  // byte address
-    static constexpr int kBytes = kColumns + 2 * kCols * (int)sizeof(Column);
-    static __device__ __forceinline__ int turn(int r) { return D % 64 == 0 ? r & 7 : (r >> 1) & 3; }
+    static constexpr int kLse = 2 * kBufB, kPos = kLse + 2 * kCols * 4, kLo = kPos + 2 * kCols * 4;  // byte addresses
+    static constexpr int kBytes = kLo + 2 * kCols * 4;
+    static __device__ __forceinline__ int turn(int r) { return D % 128 == 0 ? r & 15 : D % 64 == 0 ? (r >> 1) & 7 : (r >> 2) & 3; }
 };
 
-__device__ __forceinline__ u32x4 lds16(uint32_t addr) { return *(const u32x4 __attribute__((address_space(3))) *)(uintptr_t)addr; }
+typedef char __attribute__((address_space(3))) LdsByte;
+__device__ __forceinline__ LdsByte *lds_at(uint32_t addr) { return (LdsByte *)(uintptr_t)addr; }
+template <typename X>
+__device__ __forceinline__ X lds_word(const LdsByte *at) { return *(const X __attribute__((address_space(3))) *)at; }
+template <typename X>
+__device__ __forceinline__ void lds_put(LdsByte *at, X x) { *(X __attribute__((address_space(3))) *)at = x; }
 
 template <int D, bool kF16>
 __global__ __launch_bounds__(kWThreads, D <= 128 ? 3 : 2) void swaa_key_weights_kernel(const KeyWeightsParams p) {
@@ -107,10 +121,9 @@ __global__ __launch_bounds__(kWThreads, D <= 128 ? 3 : 2) void swaa_key_weights_
     if (k0 >= nk) return;
     const int P = p.n_prompts ? max(p.n_prompts[it.b], 0) : p.P;
     const SeenBy seen = seen_by(k0, min(k0 + kKeyTile, nk), nq, nk, p.W, p.S, P);
-    const unsigned all_cols = (unsigned)seen.n_all * (unsigned)p.G;
-    const unsigned c_begin = (unsigned)it.chunk * (unsigned)p.chunk_cols;
-    if (it.chunk > 0 && c_begin >= all_cols) return;
-    const unsigned c_end = min(all_cols, c_begin + (unsigned)p.chunk_cols);
+    const Columns<kCols> cols(seen.n_all, p.G);
+    const int s_begin = it.chunk * p.chunk_stages * (64 / kCols), s_end = min(cols.stages, s_begin + p.chunk_stages * (64 / kCols));
+    if (it.chunk > 0 && s_begin >= s_end) return;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -138,101 +151,146 @@ __global__ __launch_bounds__(kWThreads, D <= 128 ? 3 : 2) void swaa_key_weights_
 #pragma unroll
     for (int m = 0; m < kM; ++m) sum[m] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // ---- columns, a stage at a time.  A wave brings kWaveCols of a stage's; lane l keeps track of the one at l % kWaveCols.
+    // ---- columns, a stage at a time; a wave brings kWaveCols of them
     const char *q_base = p.q.ptr + 2 * ((packed ? 0 : it.b * p.q.sb) + it.kvh * (long long)p.G * p.q.sh +
                                         (packed ? p.seq.cu_q[it.b] * p.q.sn : 0));
     const float *lse_base = p.lse + (packed ? p.seq.cu_q[it.b] : it.b * p.lse_sb) + it.kvh * (long long)p.G * p.lse_sh;
-    const unsigned n_all = (unsigned)seen.n_all;
-    unsigned col = c_begin + (unsigned)(wave * kWaveCols + lane % kWaveCols), head = 0, index = 0;  // index: of the head's rows that see the tile
-    if (c_begin < c_end) {
-        head = min(col, c_end - 1) / n_all;
-        index = min(col, c_end - 1) - head * n_all;
-    }
-    float lse = 0.f;
-    int row = 0;
-    auto issue_stage = [&](int buf) {
-        row = seen.row((int)index);
-        const long long at = (long long)head * p.q.sh + (long long)row * p.q.sn;
-        lse = lse_base[head * p.lse_sh + row];
+    const int off = nk - nq;
+    // (of instruction i: row 64 i + lane of kChunks chunks each of the wave's columns, chunk of LDS, and its address behind row 0's)
+    uint32_t copy_at[kCopies];
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-            const int id = 64 * i + lane, r = id / kChunks, c = id % kChunks;  // row of the wave's, chunk of LDS
-            if (kWaveCols * kChunks % 64 != 0 && id >= kWaveCols * kChunks) break;
-            const long long of_row = ((long long)__shfl((int)(at >> 32), r) << 32) | (unsigned)__shfl((int)at, r);
-            const char *src = q_base + 2 * of_row + 16 * (c ^ T::turn(wave * kWaveCols + r));
-            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src),
-                         "s"((uint32_t)(buf * T::kBufB + wave * kWaveCols * T::kRowB + 1024 * i))
-                         : "memory");
+    for (int i = 0; i < kCopies; ++i) {
+        const int id = 64 * i + lane, c = wave * kWaveCols + id / kChunks;
+        copy_at[i] = (uint32_t)(c * (int)p.q.sn * 2 + 16 * (id % kChunks ^ T::turn(c)));
+    }
+    int head = 0, index = 0;  // of the stage: its first column
+    auto go_to = [&](int stage) {
+        head = cols.by_head ? stage / cols.per_head : 0;
+        index = kCols * (stage - (cols.by_head ? head * cols.per_head : 0));
+    };
+    // Rows of consecutive places in memory, all there: the usual stage.  row0: the first.
+    int row0 = 0;
+    bool straight = false;
+    int valid = 0;  // columns of the stage
+    float lse = 0.f;
+    int pos = 0;
+    auto issue_stage = [&](int buf) {
+        valid = min(kCols, (cols.by_head ? seen.n_all : seen.n_all * p.G) - index);
+        straight = cols.by_head && valid == kCols && (index + kCols <= seen.n || index >= seen.n);
+        row0 = seen.row(index);
+        const uint32_t to = (uint32_t)(buf * T::kBufB + wave * kWaveCols * T::kRowB);
+        const int mine = wave * kWaveCols + lane % kWaveCols;
+        if (straight) {
+            const char *src = q_base + 2 * (head * p.q.sh + row0 * p.q.sn);
+            lse = (lse_base + head * p.lse_sh + row0)[mine];
+            pos = off + row0 + mine;
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                if (kWaveCols * kChunks % 64 != 0 && 64 * i + lane >= kWaveCols * kChunks) break;
+                asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(copy_at[i]), "s"(src), "s"(to + 1024 * i) : "memory");
+            }
+        } else {
+            // column c of the stage; those behind the last one repeat it
+            auto locate = [&](int c, int &h, int &r) {
+                c = index + min(c, valid - 1);
+                h = cols.by_head ? head : c / seen.n_all;
+                r = seen.row(cols.by_head ? c : c - h * seen.n_all);
+            };
+            int h, r, lane_here = lane;
+            asm volatile("" : "+v"(lane_here));  // (what this path needs is worked out here: kept from before the loop it would cost the other one its registers)
+            locate(wave * kWaveCols + lane_here % kWaveCols, h, r);
+            lse = lse_base[h * p.lse_sh + r];
+            pos = mine < valid ? off + r : -1;
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                const int id = 64 * i + lane_here, c = wave * kWaveCols + id / kChunks;
+                if (kWaveCols * kChunks % 64 != 0 && id >= kWaveCols * kChunks) break;
+                locate(c, h, r);
+                const char *src = q_base + 2 * (h * p.q.sh + r * p.q.sn) + 16 * (id % kChunks ^ T::turn(c));
+                asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(to + 1024 * i) : "memory");
+            }
         }
     };
     auto put_columns = [&](int buf) {
-        Column c;
-        const int pos = nk - nq + row;
+        LdsByte *const at = lds_at((uint32_t)(T::kLse + 4 * (buf * kCols + wave * kWaveCols + lane)));
         // (a row whose scores are all -infinity gives no weight)
-        const bool none = col >= c_end || opaque_bits(lse) == 0xff800000u;
-        c.lse2 = none ? 0.f : lse * 1.44269504088896340736f;
-        c.pos = none ? -1 : pos;
-        c.lo = pos >= P ? -1 : pos - p.W;
-        c.pad = 0;
-        if (lane < kWaveCols)
-            *(u32x4 __attribute__((address_space(3))) *)(uintptr_t)(uint32_t)(T::kColumns + (buf * kCols + wave * kWaveCols + lane) * (int)sizeof(Column)) =
-                __builtin_bit_cast(u32x4, c);
-    };
-    auto next_columns = [&]() {  // kCols columns on; behind the last one, it again
-        col += kCols;
-        if (col >= c_end) return;
-        index += kCols;
-        if (index >= n_all) {
-            const unsigned more = n_all >= (unsigned)kCols ? 1u : index / n_all;
-            head += more;
-            index -= more * n_all;
+        const bool none = pos < 0 || opaque_bits(lse) == 0xff800000u;
+        if (lane < kWaveCols) {
+            lds_put<float>(at, none ? INFINITY : lse * 1.44269504088896340736f);
+            lds_put<int>(at + (T::kPos - T::kLse), none ? -1 : pos);
+            lds_put<int>(at + (T::kLo - T::kLse), pos >= P ? -1 : pos - p.W);
         }
     };
 
-    const uint32_t q_lane = (uint32_t)(l16 * T::kRowB);
-    if (c_begin < c_end) {
+    // S of 16 columns, whose operands lie at `at`[k-step] + offset
+    uint32_t q_at[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) q_at[ks] = (uint32_t)(l16 * T::kRowB + (((4 * ks + quad) ^ T::turn(l16)) << 4));
+    auto products = [&](LdsByte *const (&at)[KS], int offset, f32x4 (&s)[kM]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < kM; ++m) s[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const u32x4 qf = lds_word<u32x4>(at[ks] + offset);
+#pragma unroll
+            for (int m = 0; m < kM; ++m) s[m] = mfma16<kF16>(kf[m][ks], qf, s[m]);
+        }
+    };
+    if (s_begin < s_end) {
+        go_to(s_begin);
         issue_stage(0);
         put_columns(0);
     }
     int buf = 0;
-    for (unsigned c0 = c_begin; c0 < c_end; c0 += kCols, buf ^= 1) {
+    for (int stage = s_begin; stage < s_end; ++stage, buf ^= 1) {
         __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0): this wave's share of the stage has landed, and it has read the one before
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();        // everybody's; and everybody is done with the one before
         asm volatile("" ::: "memory");
-        const bool more = c0 + kCols < c_end;
+        // do all the stage's columns see all the wave's keys?
+        const int pos0 = off + row0, pos1 = pos0 + kCols - 1;
+        const bool all = straight && pos0 >= wk0 + kWaveKeys - 1 && (pos0 >= P || min(pos1, P - 1) - p.W < wk0 || wk0 + kWaveKeys <= p.S);
+        // does any of them see any?  (Rows at the edges of the tile's window; beside the sinks, the tile's other waves.)
+        const bool none = straight && (pos1 < wk0 || (pos1 < P && pos0 - p.W >= wk0 + kWaveKeys - 1 && wk0 >= p.S));
+        const int units = none ? 0 : (valid + 15) / 16;
+        const bool more = stage + 1 < s_end;
         if (more) {
-            next_columns();
+            index += kCols;
+            if (cols.by_head && index >= seen.n_all) {
+                index = 0;
+                ++head;
+            }
             issue_stage(buf ^ 1);
         }
-        const int units = (int)min((unsigned)(kCols / 16), (c_end - c0 + 15) / 16);
-        const uint32_t q_at = (uint32_t)(buf * T::kBufB) + q_lane, col_at = (uint32_t)(T::kColumns + (buf * kCols + l16) * (int)sizeof(Column));
-        for (int t = 0; t < units; ++t) {
-            const Column cl = __builtin_bit_cast(Column, lds16(col_at + (uint32_t)(16 * t * (int)sizeof(Column))));
-            f32x4 s[kM];
+        LdsByte *at[KS], *const col_at = lds_at((uint32_t)(T::kLse + 4 * (buf * kCols + l16)));
 #pragma unroll
-            for (int m = 0; m < kM; ++m) s[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int ks = 0; ks < KS; ++ks) at[ks] = lds_at(q_at[ks] + (uint32_t)(buf * T::kBufB));
+        if (all) {
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const u32x4 qf = lds16(q_at + (uint32_t)(16 * t * T::kRowB) + (uint32_t)(((4 * ks + quad) ^ T::turn(l16)) << 4));
-#pragma unroll
-                for (int m = 0; m < kM; ++m) s[m] = mfma16<kF16>(kf[m][ks], qf, s[m]);
-            }
-            // (does every column of the tile see all the wave's keys?)
-            const bool all = cl.pos >= wk0 + kWaveKeys - 1 && (cl.lo < wk0 || wk0 + kWaveKeys <= p.S);
-            if (__ballot(all) == ~0ull) {
+            for (int t = 0; t < kCols / 16; ++t) {
+                f32x4 s[kM];
+                const float lse2 = lds_word<float>(col_at + 64 * t);
+                products(at, 16 * t * T::kRowB, s);
 #pragma unroll
                 for (int m = 0; m < kM; ++m)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[m][e] += __builtin_amdgcn_exp2f(s[m][e] * p.scale_log2 - cl.lse2);
-            } else {
+                    for (int e = 0; e < 4; ++e) sum[m][e] += __builtin_amdgcn_exp2f(s[m][e] * p.scale_log2 - lse2);
+            }
+        } else {
+            for (int t = 0; t < units; ++t) {
+                const float lse2 = lds_word<float>(col_at + 64 * t);
+                const int cpos = lds_word<int>(col_at + 64 * t + (T::kPos - T::kLse)), clo = lds_word<int>(col_at + 64 * t + (T::kLo - T::kLse));
+                f32x4 s[kM];
+                products(at, 16 * t * T::kRowB, s);
+                int first = wk0 + 4 * quad;
+                asm volatile("" : "+v"(first));  // (as above)
 #pragma unroll
                 for (int m = 0; m < kM; ++m)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int key = wk0 + 16 * m + 4 * quad + e;
-                        const bool sees = key <= cl.pos && (key > cl.lo || key < p.S);
-                        const float x = __builtin_amdgcn_exp2f(s[m][e] * p.scale_log2 - cl.lse2);
+                        const int key = first + 16 * m + e;
+                        const bool sees = key <= cpos && (key > clo || key < p.S);
+                        const float x = __builtin_amdgcn_exp2f(s[m][e] * p.scale_log2 - lse2);
                         sum[m][e] += sees ? x : 0.f;
                     }
             }
@@ -278,7 +336,9 @@ __global__ __launch_bounds__(kKeyTile) void swaa_key_weights_merge_kernel(const 
     if (key >= nk) return;
     const int P = p.n_prompts ? max(p.n_prompts[b], 0) : p.P;
     const SeenBy seen = seen_by(k0, min(k0 + kKeyTile, nk), nq, nk, p.W, p.S, P);
-    const long long all_cols = (long long)seen.n_all * p.G;
+    const bool narrow = stage_cols(p.D) == 32;
+    const int stages = narrow ? Columns<32>(seen.n_all, p.G).stages : Columns<64>(seen.n_all, p.G).stages;
+    const int of_chunk = p.chunk_stages * (narrow ? 2 : 1);
     const bool has_sinks = (int)tile < p.sink_tiles;
     // its first chunk's place among the pair's items, and from chunk to chunk
     const long long first = has_sinks ? (long long)tile * p.sink_chunks : p.sink_items + ((long long)tile - p.sink_tiles);
@@ -286,7 +346,7 @@ __global__ __launch_bounds__(kKeyTile) void swaa_key_weights_merge_kernel(const 
     const int chunks = has_sinks ? p.sink_chunks : p.chunks;
     const float *src = p.partial + (first * p.pairs + pair) * kKeyTile + threadIdx.x;
     float x = src[0];
-    for (int c = 1; c < chunks && c * p.chunk_cols < all_cols; ++c) x += src[c * step];
+    for (int c = 1; c < chunks && c * of_chunk < stages; ++c) x += src[c * step];
     float *w = p.weights + b * p.w_sb + kvh * p.w_sh + key;
     *w = p.decay != 0.f ? p.decay * *w + x : x;
 }
@@ -315,20 +375,21 @@ bool plan_key_weights(KeyWeightsParams &p) {
     const int Nq = p.seq.Nq, Nk = p.seq.Nk;
     p.pairs = p.seq.B * (p.Hq / p.G);
     p.tiles = (Nk + kKeyTile - 1) / kKeyTile;
-    const long long most = (long long)p.G * Nq;
-    if (most > 0x7fffffffLL - 2 * kMinChunk) return false;
+    if ((long long)p.G * (Nq + 64LL) > 0x3fffffffLL) return false;
+    // stages (of 64 columns) of a tile seen by n rows, at most
+    auto stages_of = [&](long long n) { return Columns<64>((int)(n < Nq ? n : Nq), p.G).stages; };
+    const int most = stages_of(Nq);
     // rows that see a tile without sinks: those of its window, and generated ones (of sequences with prompt lengths of their own: maybe all)
     const long long generated = p.n_prompts ? Nk : Nk - p.P;
     const long long of_window = (long long)p.W + kKeyTile - 1 + generated;
-    const long long usual = (long long)p.G * (of_window < Nq ? of_window : Nq);
+    const int usual = stages_of(of_window);
     p.sink_tiles = usual < most ? (p.S + kKeyTile - 1) / kKeyTile : 0;
     const bool ramp = of_window >= Nq && Nq > kKeyTile;  // (a whole prompt's rows: the last tiles see few)
-    const long long all = p.pairs * ((p.tiles - p.sink_tiles) * (ramp ? usual / 2 + 1 : usual) + p.sink_tiles * most);
-    long long chunk = (all + kFillItems - 1) / kFillItems;
-    chunk = chunk > kMinChunk ? chunk : kMinChunk;
-    p.chunk_cols = (chunk + 63) / 64 * 64;
-    p.chunks = (int)((usual + p.chunk_cols - 1) / p.chunk_cols);
-    p.sink_chunks = (int)((most + p.chunk_cols - 1) / p.chunk_cols);
+    const long long all = p.pairs * ((long long)(p.tiles - p.sink_tiles) * (ramp ? usual / 2 + 1 : usual) + (long long)p.sink_tiles * most);
+    const long long chunk = (all + kFillItems - 1) / kFillItems;
+    p.chunk_stages = (int)(chunk > kMinChunk / 64 ? chunk : kMinChunk / 64);
+    p.chunks = (usual + p.chunk_stages - 1) / p.chunk_stages;
+    p.sink_chunks = (most + p.chunk_stages - 1) / p.chunk_stages;
     p.sink_items = p.sink_tiles * p.sink_chunks;
     p.items = (long long)p.pairs * (p.sink_items + (long long)(p.tiles - p.sink_tiles) * p.chunks);
     if (p.items > 0x7fffffffLL) return false;
