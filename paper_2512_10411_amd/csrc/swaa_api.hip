@@ -650,7 +650,8 @@ int swaa_cache_evict(const swaa_evict_args *a) {
     for (const void *ptr : {(const void *)a->weights, (const void *)a->kept, (const void *)a->new_lens, (const void *)a->seq_lens})
         if (misaligned_words(ptr)) return SWAA_ERR_ALIGN;
     if ((a->Hkv > 1 && a->weights_stride_h < a->Nk) || (a->B > 1 && a->weights_stride_b < a->Nk)) return SWAA_ERR_SHAPE;
-    if ((long long)a->B * a->Hkv > 0x7fffffffLL / 256) return SWAA_ERR_SHAPE;
+    if ((long long)a->B * a->Hkv > 0x7fffffffLL / 256 || a->Nk > (1 << 28) || a->B * (long long)a->Hkv * (a->n_keep / 32 + 1LL) > 0x3fffffffLL)
+        return SWAA_ERR_SHAPE;  // (one launch; weights of a head below 2 GiB)
     p.k = rows_of(a->k);
     p.v = rows_of(a->v);
     p.weights = a->weights;

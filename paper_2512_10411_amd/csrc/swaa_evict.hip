@@ -17,44 +17,43 @@ namespace {
 
 constexpr int kSThreads = 1024;
 constexpr int kSWaves = kSThreads / 64;
-constexpr int kSegment = 256;                             // rows of a wave's step, four to a lane
-constexpr int kStep = kSWaves * kSegment;                 // rows of a workgroup's step
-constexpr int kSteps = 8;                                 // steps of a round, whose weights are in registers
-constexpr int kRound = kSteps * kStep;
-constexpr int kBins = 2048;
-constexpr int kCopies = 4;                                // of the bins: lanes of equal weights seldom meet in one
+constexpr int kSegment = 256;              // rows of a wave's step, four to a lane
+constexpr int kStep = kSWaves * kSegment;  // rows of a workgroup's step
+constexpr int kBins = 2048, kDigitBits = 11;
+constexpr int kCopies = 4;                 // of the bins, side by side: lanes of equal weights seldom meet in one, nor in a bank
+constexpr int kFew = 256;                  // candidates that are ranked one against the other
 
-// Weights as whole numbers of the same order: -0 is 0, everything that is not a number weighs most.  (On the bits: the build does
-// not honour NaNs.)
+// Rows as whole numbers that the heaviest ones have the largest of: a weight's bits in its order (-0 is 0, everything that is not a
+// number weighs most), above them the rows that stay in any case, and 0 where there is no row.  (On the bits: the build does not
+// honour NaNs.)
+constexpr unsigned kPinned = ~0u, kNotANumber = ~0u - 1u;
 __device__ __forceinline__ unsigned order_of(unsigned bits) {
-    if ((bits & 0x7fffffffu) > 0x7f800000u) return ~0u;
+    if ((bits & 0x7fffffffu) > 0x7f800000u) return kNotANumber;
     if (bits == 0x80000000u) bits = 0;
     return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
 }
 
-// Exclusive sum over the workgroup's threads of x; `all`: of all of them.
+// Exclusive sum over the workgroup's threads of x; `all`: of all of them.  Callers have a barrier between two calls.
 __device__ __forceinline__ unsigned block_exclusive(unsigned x, unsigned *scratch, unsigned &all) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const unsigned incl = wave_inclusive_scan(x);
     if (lane == 63) scratch[wave] = incl;
     __syncthreads();
-    unsigned before = 0;
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < kSWaves; ++w) {
-        const unsigned n = scratch[w];
-        before += w < wave ? n : 0u;
-        all += n;
-    }
-    __syncthreads();
+    const unsigned waves = wave_inclusive_scan(lane < kSWaves ? scratch[lane] : 0u);
+    all = wave_read_lane(waves, kSWaves - 1);
+    const unsigned before = wave ? wave_read_lane(waves, wave - 1) : 0u;
     return before + incl - x;
 }
 
+// kSteps: steps of a round, whose rows' orders are in registers; longer sequences take several rounds and read their weights once
+// more for each look at them.
+template <int kSteps>
 __global__ __launch_bounds__(kSThreads) void swaa_evict_select_kernel(const EvictParams p) {
-    __shared__ unsigned bins[kCopies][kBins];
-    __shared__ unsigned scratch[kSWaves], found[2];
+    constexpr int kRound = kSteps * kStep;
+    __shared__ __attribute__((aligned(16))) unsigned bins[kBins * kCopies];
+    __shared__ unsigned scratch[kSWaves], scratch2[kSWaves], found[4];
     __shared__ unsigned heavier[kSteps * kSWaves], equal[kSteps * kSWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const unsigned pair = blockIdx.x, b = fastdiv(pair, p.div_hkv), kvh = pair - b * (unsigned)p.Hkv;
     const int n = p.seq_lens ? max(min(p.seq_lens[b], p.Nk), 0) : p.Nk;
     int *kept = p.kept + (long long)pair * p.n_keep;
@@ -62,89 +61,125 @@ __global__ __launch_bounds__(kSThreads) void swaa_evict_select_kernel(const Evic
         for (int i = tid; i < p.n_keep; i += kSThreads) kept[i] = i < n ? i : -1;
         return;
     }
-    float *weights = p.weights + b * p.w_sb + kvh * p.w_sh;
-    const unsigned *bits_of = reinterpret_cast<const unsigned *>(weights);
-    const int lo = p.n_sink, hi = n - p.n_recent;                          // rows that are judged
-    const unsigned wanted = (unsigned)(p.n_keep - p.n_sink - p.n_recent);  // of which stay (fewer than there are)
-    const int rounds = (n + kRound - 1) / kRound;
+    // (a buffer of n words: what is read behind them is 0, without a branch around the read)
+    const __amdgpu_buffer_rsrc_t words = __builtin_amdgcn_make_buffer_rsrc(p.weights + b * p.w_sb + kvh * p.w_sh, 0, 4 * n, 0x00027000);
+    const int lo = p.n_sink, hi = n - p.n_recent, rounds = (n + kRound - 1) / kRound;
 
-    // element e (0 .. 3) of step s of a round: row round * kRound + s * kStep + wave * kSegment + 64 e + lane
-    unsigned raw[kSteps][4];
-    auto row_of = [&](int round, int s, int e) { return round * kRound + s * kStep + wave * kSegment + 64 * e + lane; };
-    auto load_round = [&](int round) {
+    // element e (0 .. 3) of step s of a round: row first_of(round, s) + 64 e + lane
+    unsigned order[kSteps][4];
+    auto first_of = [&](int round, int s) { return round * kRound + s * kStep + wave * kSegment; };
+    auto load_round = [&](int round) __attribute__((always_inline)) {
+        int l = lane;
+        asm volatile("" : "+v"(l));  // (what depends on it is worked out here: kept from one look to the next it would need the registers)
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = row_of(round, s, e);
-                raw[s][e] = i < n ? bits_of[i] : 0u;
+            for (int e = 0; e < 4; ++e) order[s][e] = __builtin_amdgcn_raw_buffer_load_b32(words, 4 * (first_of(round, s) + 64 * e + l), 0, 0);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int first = first_of(round, s);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) order[s][e] = order_of(order[s][e]);
+            if (first < lo || first + kSegment > hi) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = first + 64 * e + l;
+                    order[s][e] = i >= n ? 0u : i < lo || i >= hi ? kPinned : order[s][e];
+                }
             }
+        }
+    };
+    // f(order) for every row
+    auto look = [&](auto f) __attribute__((always_inline)) {
+        for (int round = 0; round < rounds; ++round) {
+            if (rounds > 1) load_round(round);
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                if (first_of(round, s) >= n) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f(order[s][e]);
+            }
+        }
     };
     load_round(0);
 
-    // ---- the least weight that stays, from its highest bits down
-    unsigned prefix = 0, mask = 0, left = wanted;  // `left`: how many of those with the prefix stay
-    if (wanted > 0) {
-        const int shifts[3] = {21, 10, 0}, widths[3] = {11, 11, 10};
-        for (int d = 0; d < 3; ++d) {
-            const int shift = shifts[d];
-            const unsigned digits = 1u << widths[d];
-            for (int i = tid; i < kCopies * kBins; i += kSThreads) bins[0][i] = 0;
+    // ---- the least order that stays, from its highest bits down, until few rows have those
+    unsigned prefix = 0, mask = 0, left = (unsigned)p.n_keep;  // `left`: how many of those with the prefix stay
+    for (int shift = 32 - kDigitBits, width = kDigitBits; mask != ~0u;) {
+        static_assert(kCopies == 4 && kBins == 2 * kSThreads, "");
+        u32x4 *const four = reinterpret_cast<u32x4 *>(bins);
+        four[tid] = four[tid + kSThreads] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+        unsigned *const mine = bins + lane % kCopies;
+        if (mask == 0)
+            look([&](unsigned u) { atomicAdd(&mine[(u >> (32 - kDigitBits)) * kCopies], 1u); });
+        else
+            look([&](unsigned u) {
+                if ((u & mask) == prefix) atomicAdd(&mine[((u >> shift) & (kBins - 1)) * kCopies], 1u);  // (the last digit has ten bits: the eleventh is the prefix's)
+            });
+        __syncthreads();
+        // thread t: bins 2047 - 2 t and the one below, the highest first
+        unsigned c[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const u32x4 copies = four[kBins - 1 - 2 * tid - k];
+            c[k] = (copies[0] + copies[1]) + (copies[2] + copies[3]);
+        }
+        unsigned all;
+        const unsigned before = block_exclusive(c[0] + c[1], scratch, all);
+        if (before < left && left <= before + c[0] + c[1]) {
+            const bool first = left <= before + c[0];
+            found[0] = kBins - 1 - 2 * tid - (first ? 0 : 1);
+            found[1] = left - before - (first ? 0 : c[0]);
+            found[2] = first ? c[0] : c[1];
+            found[3] = 0;
+        }
+        __syncthreads();
+        prefix |= found[0] << shift;
+        mask |= ((1u << width) - 1) << shift;
+        left = found[1];
+        const unsigned candidates = found[2];
+        if (candidates <= (unsigned)kFew && mask != ~0u) {
+            // each of them against all others
+            unsigned *const few = bins;
+            look([&](unsigned u) {
+                if ((u & mask) == prefix) few[atomicAdd(&found[3], 1u)] = u;
+            });
             __syncthreads();
-            for (int round = 0; round < rounds; ++round) {
-                if (rounds > 1) load_round(round);
-#pragma unroll
-                for (int s = 0; s < kSteps; ++s) {
-                    if (round * kRound + s * kStep >= hi) break;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = row_of(round, s, e);
-                        const unsigned u = order_of(raw[s][e]);
-                        if (i >= lo && i < hi && (u & mask) == prefix) atomicAdd(&bins[lane % kCopies][(u >> shift) & (digits - 1)], 1u);
-                    }
+            if (tid < (int)candidates) {
+                const unsigned u = few[tid];
+                unsigned above = 0, same = 0;
+                for (unsigned i = 0; i < candidates; ++i) {
+                    above += few[i] > u;
+                    same += few[i] == u;
+                }
+                if (above < left && left <= above + same) {  // (every thread that holds it says the same)
+                    found[0] = u;
+                    found[1] = left - above;
                 }
             }
             __syncthreads();
-            // thread t: digits digits - 1 - 2 t and the one below, the highest first
-            unsigned c[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int digit = (int)digits - 1 - 2 * tid - k;
-                c[k] = 0;
-                if (digit >= 0)
-#pragma unroll
-                    for (int copy = 0; copy < kCopies; ++copy) c[k] += bins[copy][digit];
-            }
-            unsigned all;
-            const unsigned before = block_exclusive(c[0] + c[1], scratch, all);
-            if (before < left && left <= before + c[0] + c[1]) {
-                const bool first = left <= before + c[0];
-                found[0] = digits - 1 - 2 * tid - (first ? 0 : 1);
-                found[1] = left - before - (first ? 0 : c[0]);
-            }
-            __syncthreads();
-            prefix |= found[0] << shift;
-            mask |= (digits - 1) << shift;
+            prefix = found[0];
             left = found[1];
-            __syncthreads();
+            mask = ~0u;
         }
+        width = shift < kDigitBits ? shift : kDigitBits;
+        shift -= width;
     }
 
-    // ---- places: stayers are the pinned rows, the heavier ones and the first `left` of the equal ones
+    // ---- places: the heavier rows stay, and the first `left` of the equal ones
     unsigned base_heavier = 0, base_equal = 0;
     for (int round = 0; round < rounds; ++round) {
         if (rounds > 1) load_round(round);
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             unsigned nh = 0, ne = 0;
+            if (first_of(round, s) < n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = row_of(round, s, e);
-                const unsigned u = order_of(raw[s][e]);
-                const bool judged = i >= lo && i < hi, pinned = i < n && !judged;
-                nh += __popcll(__ballot(pinned || (wanted > 0 && judged && u > prefix)));
-                ne += __popcll(__ballot(wanted > 0 && judged && u == prefix));
-            }
+                for (int e = 0; e < 4; ++e) {
+                    nh += __popcll(__ballot(order[s][e] > prefix));
+                    ne += __popcll(__ballot(order[s][e] == prefix));
+                }
             if (lane == 0) {
                 heavier[s * kSWaves + wave] = nh;
                 equal[s * kSWaves + wave] = ne;
@@ -155,7 +190,7 @@ __global__ __launch_bounds__(kSThreads) void swaa_evict_select_kernel(const Evic
         const bool has = tid < kSteps * kSWaves;
         unsigned all_heavier, all_equal;
         const unsigned eh = block_exclusive(has ? heavier[tid] : 0u, scratch, all_heavier);
-        const unsigned ee = block_exclusive(has ? equal[tid] : 0u, scratch, all_equal);
+        const unsigned ee = block_exclusive(has ? equal[tid] : 0u, scratch2, all_equal);
         if (has) {
             heavier[tid] = eh;
             equal[tid] = ee;
@@ -163,92 +198,219 @@ __global__ __launch_bounds__(kSThreads) void swaa_evict_select_kernel(const Evic
         __syncthreads();
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            if (round * kRound + s * kStep >= n) break;
+            const int first = first_of(round, s);
+            if (first >= n) break;
             unsigned h = base_heavier + heavier[s * kSWaves + wave], q = base_equal + equal[s * kSWaves + wave];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int i = row_of(round, s, e);
-                const unsigned u = order_of(raw[s][e]);
-                const bool judged = i >= lo && i < hi, pinned = i < n && !judged;
-                const bool is_heavier = pinned || (wanted > 0 && judged && u > prefix), is_equal = wanted > 0 && judged && u == prefix;
-                const unsigned long long bh = __ballot(is_heavier), bq = __ballot(is_equal);
-                const unsigned long long below = (1ull << lane) - 1ull;
-                const unsigned my_h = h + __popcll(bh & below), my_q = q + __popcll(bq & below);
-                if (is_heavier || (is_equal && my_q < left)) {
-                    const unsigned place = my_h + min(my_q, left);
-                    kept[place] = i;
-                    // (a row moves down at most: in this round the weights are in registers, and earlier ones have been read)
-                    weights[place] = __uint_as_float(raw[s][e]);
+                const unsigned u = order[s][e];
+                const unsigned long long bh = __ballot(u > prefix), bq = __ballot(u == prefix);
+                unsigned place = h + min(q, left) + __builtin_amdgcn_mbcnt_hi((unsigned)(bh >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)bh, 0u));
+                bool stays = u > prefix;
+                if (bq) {
+                    const unsigned my_q = q + __builtin_amdgcn_mbcnt_hi((unsigned)(bq >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)bq, 0u));
+                    place += min(my_q, left) - min(q, left);
+                    stays = stays || (u == prefix && my_q < left);
+                    q += __popcll(bq);
                 }
+                if (stays) kept[place] = first + 64 * e + lane;
                 h += __popcll(bh);
-                q += __popcll(bq);
             }
         }
         base_heavier += all_heavier;
         base_equal += all_equal;
         __syncthreads();
     }
-    for (int i = p.n_keep + tid; i < n; i += kSThreads) weights[i] = 0.f;
 }
 
-constexpr int kMThreads = 256;
-constexpr int kMRows = 8;  // of a thread, on the way at a time
+constexpr int kMThreads = 1024;
+constexpr int kMRows = 4;  // of a thread, on the way at a time; those of the next block are asked for before they are written
 
-// kLanes: lanes of 16 bytes that make a slice of a row.
-template <int kLanes>
-__global__ __launch_bounds__(kMThreads) void swaa_evict_move_kernel(const EvictParams p, int slices) {
-    constexpr int kStride = kMThreads / kLanes;
-    const int tid = threadIdx.x;
-    // pairs in turn: the slices of a row share a die's L2 (where the pairs are a multiple of the dies)
-    const unsigned pairs = (unsigned)(p.B * p.Hkv), pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-    const int slice = (int)(rest % (unsigned)slices), of_v = (int)(rest / (unsigned)slices);
-    const unsigned b = fastdiv(pair, p.div_hkv), kvh = pair - b * (unsigned)p.Hkv;
-    if (rest == 0 && kvh == 0 && tid == 0 && p.new_lens) {
-        // (no other thread of this kernel reads the lengths: they may be the same array)
-        const int n = p.seq_lens ? max(min(p.seq_lens[b], p.Nk), 0) : p.Nk;
-        p.new_lens[b] = min(n, p.n_keep);
-    }
-    const Rows &t = of_v ? p.v : p.k;
-    const int *kept = p.kept + (long long)pair * p.n_keep;
-    const int chunk = slice * kLanes + tid % kLanes;
-    const bool in_row = 8 * chunk < p.D;
-    const int limit = min(p.n_keep, p.Nk);
-    for (int first = p.n_sink; first < limit; first += kMRows * kStride) {
-        u32x4 data[kMRows];
-        char *dst[kMRows];
+// Moves rows kept[i] to i for i in [begin, end), in that order as far as anyone can see: a block's rows are read, in all threads,
+// before any of them is written, and the next block's come from behind those that this one writes.  Ends at the first row that comes
+// from `split` or behind it (`kept` ascends).  kPerRow threads share a row; place(i) says where row i stands (elements of Data, negative: nowhere, and whether it may be written there).
+template <int kPerRow, typename Data, typename Place>
+__device__ __forceinline__ void move_rows(const int *kept, int begin, int end, int split, bool takes_part, Data *base, Place place) {
+    constexpr int kStride = kMThreads / kPerRow, kBlock = kMRows * kStride;
+    int from[kMRows];                    // of a block: the rows that come, -1 where none does,
+    long long src[kMRows], dst[kMRows];  // and both ends (-1: none)
+    Data data[kMRows] = {};
+    auto row_of = [&](int first, int r) { return first + r * kStride + (int)threadIdx.x / kPerRow; };
+    auto load_from = [&](int first) {
 #pragma unroll
         for (int r = 0; r < kMRows; ++r) {
-            const int i = first + r * kStride + tid / kLanes;
-            const int from = i < limit && in_row ? kept[i] : -1;
-            dst[r] = nullptr;
-            data[r] = u32x4{0, 0, 0, 0};
-            if (from > i) {
+            const int i = row_of(first, r);
+            from[r] = i < end && takes_part ? kept[i] : -1;
+            if (from[r] >= split) from[r] = -1;
+        }
+    };
+    auto find = [&](int first) {
+#pragma unroll
+        for (int r = 0; r < kMRows; ++r) {
+            const int i = row_of(first, r);
+            src[r] = dst[r] = -1;
+            if (from[r] > i) {
                 bool inside, unused;
-                const long long at = cache_row(p.pages, t, (int)b, 0, i, false, inside), src = cache_row(p.pages, t, (int)b, 0, from, false, unused);
-                char *base = t.ptr + 2 * (kvh * t.sh + 8 * chunk);
-                if (inside) dst[r] = base + 2 * at;
-                data[r] = *reinterpret_cast<const u32x4 *>(base + 2 * src);
+                const long long to = place(i, inside);
+                src[r] = place(from[r], unused);
+                if (inside) dst[r] = to;
             }
         }
-        // every read of this block of rows is done, in all waves, before the first write
-#pragma unroll
-        for (int r = 0; r < kMRows; ++r) asm volatile("" ::"v"(data[r]));
-        __syncthreads();
+    };
+    auto load_data = [&]() {
 #pragma unroll
         for (int r = 0; r < kMRows; ++r)
-            if (dst[r]) *reinterpret_cast<u32x4 *>(dst[r]) = data[r];
+            if (src[r] >= 0) data[r] = base[src[r]];
+    };
+    load_from(begin);
+    find(begin);
+    load_data();
+    load_from(begin + kBlock);
+    int comes = begin < end ? kept[begin] : 0;  // the first row of the block
+    for (int first = begin; first < end && comes < split; first += kBlock) {
+        comes = kept[min(first + kBlock, end - 1)];
+        Data now[kMRows];
+        long long to[kMRows];
+#pragma unroll
+        for (int r = 0; r < kMRows; ++r) {
+            now[r] = data[r];
+            to[r] = dst[r];
+            asm volatile("" : "+v"(now[r]));  // (waits for it)
+        }
+        __syncthreads();
+        find(first + kBlock);
+        load_data();
+#pragma unroll
+        for (int r = 0; r < kMRows; ++r)
+            if (to[r] >= 0) base[to[r]] = now[r];
+        load_from(first + 2 * kBlock);
     }
+}
+
+// kLanes: lanes of 16 bytes that make a slice of a row of K or V.  One workgroup of a pair moves its weights.
+// Rows that come from `split` or behind it are left to the kernel below.
+template <int kLanes>
+__global__ __launch_bounds__(kMThreads) void swaa_evict_move_kernel(const EvictParams p, int slices, int split) {
+    const int tid = threadIdx.x;
+    // pairs in turn: the slices of a row share a die's L2 (where the pairs are a multiple of the dies)
+    const unsigned pairs = (unsigned)(p.B * p.Hkv), pair = blockIdx.x % pairs, part = blockIdx.x / pairs;
+    const unsigned b = fastdiv(pair, p.div_hkv), kvh = pair - b * (unsigned)p.Hkv;
+    const int *kept = p.kept + (long long)pair * p.n_keep;
+    const int begin = p.n_sink, end = min(p.n_keep, p.Nk);
+    if (part == 0) {
+        float *weights = p.weights + b * p.w_sb + kvh * p.w_sh;
+        move_rows<1>(kept, begin, end, p.Nk, true, weights, [](int i, bool &inside) {
+            inside = true;
+            return (long long)i;
+        });
+        __syncthreads();  // (its reads are done)
+        const int n = p.seq_lens ? max(min(p.seq_lens[b], p.Nk), 0) : p.Nk;
+        for (int i = p.n_keep + tid; i < n; i += kMThreads) weights[i] = 0.f;
+        if (p.new_lens && kvh == 0 && tid == 0) p.new_lens[b] = min(n, p.n_keep);
+        return;
+    }
+    const Rows &t = part > (unsigned)slices ? p.v : p.k;
+    const int chunk = (int)((part - 1) % (unsigned)slices) * kLanes + tid % kLanes;
+    move_rows<kLanes>(kept, begin, end, split, 8 * chunk < p.D, reinterpret_cast<u32x4 *>(t.ptr + 2 * (kvh * t.sh + 8 * chunk)), [&](int i, bool &inside) {
+        return cache_row(p.pages, t, (int)b, 0, i, false, inside) / 8;  // (strides are multiples of 8 elements)
+    });
+}
+
+// Rows from behind the first n_keep: nothing is written where they stand, so they move in any order.  Rows of K, then of V.
+constexpr int kFThreads = 256, kFRows = 4;  // (rows of a thread)
+template <int kPerRow>
+__global__ __launch_bounds__(kFThreads) void swaa_evict_far_kernel(const EvictParams p, int blocks) {
+    constexpr int kStride = kFThreads / kPerRow;
+    const unsigned pairs = (unsigned)(p.B * p.Hkv), pair = blockIdx.x % pairs, part = blockIdx.x / pairs;
+    const unsigned b = fastdiv(pair, p.div_hkv), kvh = pair - b * (unsigned)p.Hkv;
+    const bool of_v = part >= (unsigned)blocks;
+    const int first = (int)(of_v ? part - (unsigned)blocks : part) * kStride * kFRows + (int)threadIdx.x / kPerRow, chunk = (int)threadIdx.x % kPerRow;
+    const Rows &t = of_v ? p.v : p.k;
+    const int *kept = p.kept + (long long)pair * p.n_keep;
+    char *const base = t.ptr + 2 * (kvh * t.sh + 8 * chunk);
+    int from[kFRows];
+    long long src[kFRows], dst[kFRows];
+    u32x4 data[kFRows];
+#pragma unroll
+    for (int r = 0; r < kFRows; ++r) {
+        const int i = first + r * kStride;
+        from[r] = i < p.n_keep && 8 * chunk < p.D ? kept[i] : -1;
+    }
+#pragma unroll
+    for (int r = 0; r < kFRows; ++r) {
+        dst[r] = -1;
+        if (from[r] >= p.n_keep) {
+            bool inside, unused;
+            const long long to = cache_row(p.pages, t, (int)b, 0, first + r * kStride, false, inside);
+            src[r] = cache_row(p.pages, t, (int)b, 0, from[r], false, unused);
+            if (inside) dst[r] = to;
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kFRows; ++r)
+        if (dst[r] >= 0) data[r] = *reinterpret_cast<const u32x4 *>(base + 2 * src[r]);
+#pragma unroll
+    for (int r = 0; r < kFRows; ++r)
+        if (dst[r] >= 0) *reinterpret_cast<u32x4 *>(base + 2 * dst[r]) = data[r];
+}
+
+// New lengths in place of the old ones: when no kernel reads those any more.
+__global__ void swaa_evict_lengths_kernel(const EvictParams p) {
+    const int b = (int)(blockIdx.x * blockDim.x + threadIdx.x);
+    if (b < p.B) p.new_lens[b] = min(max(min(p.seq_lens[b], p.Nk), 0), p.n_keep);
+}
+
+template <int kSteps>
+void select(const EvictParams &p, hipStream_t stream) {
+    swaa_evict_select_kernel<kSteps><<<dim3((unsigned)(p.B * p.Hkv)), dim3(kSThreads), 0, stream>>>(p);
+}
+template <int kLanes>
+void move(const EvictParams &p, int split, hipStream_t stream) {
+    const int slices = (p.D / 8 + kLanes - 1) / kLanes;
+    swaa_evict_move_kernel<kLanes><<<dim3((unsigned)(p.B * p.Hkv) * (1 + 2 * (unsigned)slices)), dim3(kMThreads), 0, stream>>>(p, slices, split);
+}
+template <int kPerRow>
+void move_far(const EvictParams &p, hipStream_t stream) {
+    constexpr int kRows = kFThreads / kPerRow * kFRows;
+    const int blocks = (p.n_keep + kRows - 1) / kRows;
+    swaa_evict_far_kernel<kPerRow><<<dim3((unsigned)(p.B * p.Hkv) * 2 * (unsigned)blocks), dim3(kFThreads), 0, stream>>>(p, blocks);
 }
 
 }  // namespace
 
-hipError_t launch_evict(const EvictParams &p, hipStream_t stream) {
-    const unsigned pairs = (unsigned)(p.B * p.Hkv);
-    swaa_evict_select_kernel<<<dim3(pairs), dim3(kSThreads), 0, stream>>>(p);
-    const hipError_t err = hipGetLastError();
+hipError_t launch_evict(const EvictParams &params, hipStream_t stream) {
+    EvictParams p = params;
+    const bool in_place = p.new_lens && p.new_lens == p.seq_lens;
+    if (in_place) p.new_lens = nullptr;
+    if (p.Nk <= kStep)
+        select<1>(p, stream);
+    else if (p.Nk <= 4 * kStep)
+        select<4>(p, stream);
+    else
+        select<16>(p, stream);
+    hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    const int lanes = 4, slices = (p.D / 8 + lanes - 1) / lanes;
-    swaa_evict_move_kernel<4><<<dim3(pairs * 2 * (unsigned)slices), dim3(kMThreads), 0, stream>>>(p, slices);
+    // Half the rows leave or more: most that stay come from behind the first n_keep.
+    const bool far = p.Nk / 2 >= p.n_keep;
+    const long long halves = (long long)p.B * p.Hkv * 2;
+    const int split = far ? p.n_keep : p.Nk;
+    if (halves * (p.D / 32) >= 256)
+        move<4>(p, split, stream);
+    else
+        move<2>(p, split, stream);
+    err = hipGetLastError();
+    if (far && err == hipSuccess) {
+        if (p.D <= 64)
+            move_far<8>(p, stream);
+        else if (p.D <= 128)
+            move_far<16>(p, stream);
+        else
+            move_far<32>(p, stream);
+    }
+    err = hipGetLastError();
+    if (err != hipSuccess || !in_place) return err;
+    p.new_lens = params.new_lens;
+    swaa_evict_lengths_kernel<<<dim3((unsigned)(p.B + 255) / 256), dim3(256), 0, stream>>>(p);
     return hipGetLastError();
 }
 
