@@ -229,7 +229,7 @@ class _NoHostCalls:
     def fwd(*args):
         return None
 
-    decode = decode_ex = fill_fwd_ex = fwd
+    decode = decode_ex = fill_fwd_ex = norm_rope = fwd
 
 
 def _native_part(torch):
@@ -244,7 +244,8 @@ def _native_part(torch):
             lib.swaa_attn_decode_ex, lib.swaa_attn_decode_ex_workspace_bytes)),
             torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
             lib.swaa_version(), ctypes.sizeof(SwaaFwdArgs), ctypes.sizeof(SwaaDecodeArgs), str(torch.__version__))
-    except (ImportError, TypeError) as e:  # (TypeError: its `bind` takes other arguments)
+        _host_calls.bind_cache(ctypes.cast(lib.swaa_qk_norm_rope, ctypes.c_void_p).value, ctypes.sizeof(SwaaNormRopeArgs))
+    except (ImportError, TypeError, AttributeError) as e:  # (TypeError: its `bind` takes other arguments; AttributeError: it lacks one)
         warnings.warn(f"{HOST_CALLS_PATH} is not used, calls take longer on the way to the library ({e}): "
                       "build it with `python -m paper_2512_10411_amd.build`", RuntimeWarning, stacklevel=4)
         return _NoHostCalls
@@ -935,6 +936,12 @@ def swaa_qk_norm_rope(q, k, inv_freq=None, positions=None, q_weight=None, k_weig
     None: Nk) or of cu_seqlens_k, their own rows included.  Returns (q_out, k_out, v_out); v_out is None without v.
     """
     tc = torch or _torch()
+    if q_out is None and stream is None:
+        r = _host.norm_rope(q, k, inv_freq, positions, q_weight, k_weight, eps, interleaved, v, k_out, v_out, cu_seqlens_q, cu_seqlens_k,
+                            max_seqlen_q, max_seqlen_k, seq_lens, block_table, total_rows_q)
+        if r is not None:
+            q_out, made = _results(r)
+            return q_out, (made if k_out is None else k_out), v_out
     packed, paged = cu_seqlens_q is not None, block_table is not None
     nd = 3 if packed else 4
     _elements(tc, q, "q", dims=nd)

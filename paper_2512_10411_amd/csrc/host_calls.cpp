@@ -284,7 +284,120 @@ PyObject *fill_fwd_ex(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses of the six entry points above, in their order, then current_device and current_stream, the library's version, the
+decltype(&swaa_qk_norm_rope) norm_rope_entry;
+
+// swaa_tensor of a view [blocks, heads, rows, D] or [heads, rows, D] (a dimension of one entry has no stride to speak of).
+swaa_tensor rows_of(const at::Tensor &t) {
+    const int64_t d = t.dim() - 3, n = t.size(d + 1);
+    return {t.data_ptr(), d && t.size(0) > 1 ? t.stride(0) : 0, t.size(d) > 1 ? t.stride(d) : 0, n > 1 ? t.stride(d + 1) : t.size(d + 2)};
+}
+// Address of a contiguous tensor of numbers of this type and shape, if it is given; false if it is anything else.
+template <typename T>
+bool plain_numbers(PyObject *o, int device, at::ScalarType dtype, at::IntArrayRef sizes, const T *&data) {
+    if (o == Py_None) return true;
+    const at::Tensor *t = plain_tensor(o, device);
+    if (!t || t->scalar_type() != dtype || t->sizes() != sizes || !t->is_contiguous()) return false;
+    data = static_cast<const T *>(t->data_ptr());
+    return true;
+}
+
+// norm_rope(q, k, inv_freq, positions, q_weight, k_weight, eps, interleaved, v, k_out, v_out, cu_seqlens_q, cu_seqlens_k, max_seqlen_q,
+// max_seqlen_k, seq_lens, block_table, total_rows_q): (q_out, k_out), the latter None if it was given
+PyObject *norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int device;
+    swaa_norm_rope_args s{};
+    if (n != 18 || !plain_call(a[0], device, s.stream)) Py_RETURN_NONE;
+    const bool packed = a[11] != Py_None, paged = a[16] != Py_None, cache = a[9] != Py_None;
+    const int64_t dims = packed ? 3 : 4;
+    const at::Tensor *q = plain_tensor(a[0], device), *k = plain_tensor(a[1], device), *t;
+    if (!q || (q->scalar_type() != at::kBFloat16 && q->scalar_type() != at::kHalf)) Py_RETURN_NONE;
+    auto like_q = [&](const at::Tensor *x, int64_t d) { return x && x->scalar_type() == q->scalar_type() && x->dim() == d && x->stride(-1) == 1 && x->size(-1) == q->size(-1); };
+    if (!like_q(q, dims) || !like_q(k, dims) || k->size(-2) != q->size(-2) || (!packed && k->size(0) != q->size(0))) Py_RETURN_NONE;
+    const int64_t D = q->size(-1), T = q->size(-2), Hkv = k->size(-3), B = packed ? 0 : q->size(0);
+    s.Hq = (int)q->size(-3), s.Hkv = (int)Hkv, s.D = (int)D;
+    if (a[2] != Py_None) {
+        t = plain_tensor(a[2], device);
+        if (!t || t->scalar_type() != at::kFloat || !t->is_contiguous()) Py_RETURN_NONE;
+        s.inv_freq = static_cast<const float *>(t->data_ptr()), s.rot_dim = (int)(2 * t->numel());
+    }
+    if ((a[4] == Py_None) != (a[5] == Py_None) || !plain_numbers(a[4], device, at::kFloat, {D}, s.q_weight) || !plain_numbers(a[5], device, at::kFloat, {D}, s.k_weight))
+        Py_RETURN_NONE;
+    if (!PyFloat_CheckExact(a[6]) || !PyBool_Check(a[7])) Py_RETURN_NONE;
+    s.eps = (float)PyFloat_AS_DOUBLE(a[6]), s.interleaved = a[7] == Py_True;
+    const at::Tensor *v = nullptr, *k_out = nullptr, *v_out = nullptr;
+    if (cache) {
+        k_out = plain_tensor(a[9], device);
+        if (!like_q(k_out, paged ? 4 : dims) || k_out->size(-3) != Hkv || (!packed && !paged && k_out->size(0) != B)) Py_RETURN_NONE;
+        if (packed && a[12] == Py_None) Py_RETURN_NONE;
+    } else if (paged || a[15] != Py_None || a[12] != Py_None) {
+        Py_RETURN_NONE;
+    }
+    if (a[8] != Py_None) {
+        v = plain_tensor(a[8], device), v_out = cache ? plain_tensor(a[10], device) : nullptr;
+        if (!like_q(v, dims) || v->sizes() != k->sizes() || !like_q(v_out, k_out ? k_out->dim() : 0) || v_out->sizes() != k_out->sizes()) Py_RETURN_NONE;
+        s.v = rows_of(*v), s.v_out = rows_of(*v_out);
+    } else if (a[10] != Py_None) {
+        Py_RETURN_NONE;
+    }
+    if (packed) {
+        const at::Tensor *cu_q, *cu_k;
+        if (!plain_vector(a[11], device, -1, cu_q) || !plain_vector(cache ? a[12] : a[11], device, cu_q->numel(), cu_k) || a[15] != Py_None) Py_RETURN_NONE;
+        s.B = (int)cu_q->numel() - 1;
+        s.cu_seqlens_q = static_cast<const int *>(cu_q->data_ptr()), s.cu_seqlens_k = static_cast<const int *>(cu_k->data_ptr());
+        if (!plain_int(a[13], s.Nq) || !plain_int(cache ? a[14] : a[13], s.Nk)) Py_RETURN_NONE;
+        s.total_rows_q = T;
+        if (a[17] != Py_None) Py_RETURN_NONE;
+    } else {
+        const int64_t rows = cache ? k_out->size(-2) : T;
+        if (a[12] != Py_None || (paged && a[14] == Py_None)) Py_RETURN_NONE;
+        s.B = (int)B, s.Nq = (int)T, s.Nk = (int)rows;
+        if (a[14] != Py_None && (!plain_int(a[14], s.Nk) || (!paged && s.Nk > rows))) Py_RETURN_NONE;
+        if (!plain_numbers(a[15], device, at::kInt, {B}, s.seq_lens)) Py_RETURN_NONE;
+    }
+    if (paged) {
+        t = plain_tensor(a[16], device);
+        if (!t || t->scalar_type() != at::kInt || t->dim() != 2 || t->size(0) != s.B || t->size(0) < 1 || (t->size(1) > 1 && t->stride(1) != 1)) Py_RETURN_NONE;
+        s.block_table = static_cast<const int *>(t->data_ptr());
+        s.block_table_stride = (int)(s.B > 1 ? t->stride(0) : t->size(1)), s.page_size = (int)k_out->size(2), s.num_pages = (int)k_out->size(0);
+    }
+    if (packed ? !plain_numbers(a[3], device, at::kInt, {T}, s.positions) : !plain_numbers(a[3], device, at::kInt, {B, T}, s.positions)) Py_RETURN_NONE;
+    s.dtype = q->scalar_type() == at::kHalf ? SWAA_F16 : SWAA_BF16;
+    const at::Tensor q_new = at::empty(q->sizes(), q->options()), k_new = cache ? at::Tensor() : at::empty(k->sizes(), k->options());
+    s.q = rows_of(*q), s.k = rows_of(*k), s.q_out = rows_of(q_new), s.k_out = rows_of(cache ? *k_out : k_new);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = norm_rope_entry(&s);
+    Py_END_ALLOW_THREADS
+    if (rc != SWAA_OK) return PyLong_FromLong(rc);
+    PyObject *pair = PyTuple_New(2);
+    if (!pair) return nullptr;
+    PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(q_new));
+    PyObject *second = cache ? Py_None : THPVariable_Wrap(k_new);
+    if (cache) Py_INCREF(second);
+    PyTuple_SET_ITEM(pair, 1, second);
+    return pair;
+    END_HANDLE_TH_ERRORS
+}
+
+// bind_cache(address of the entry point above, size of the binding's argument block), behind bind, which has checked the library.
+PyObject *bind_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 2) {
+        PyErr_SetString(PyExc_TypeError, "bind_cache takes an address and a number");
+        return nullptr;
+    }
+    void *at = PyLong_AsVoidPtr(a[0]);
+    const long long bytes = PyErr_Occurred() ? -1 : PyLong_AsLongLong(a[1]);
+    if (PyErr_Occurred()) return nullptr;
+    if (bytes != (long long)sizeof(swaa_norm_rope_args)) {
+        PyErr_Format(PyExc_ImportError, "compiled for an argument block of %zu bytes, not %lld", sizeof(swaa_norm_rope_args), bytes);
+        return nullptr;
+    }
+    norm_rope_entry = reinterpret_cast<decltype(norm_rope_entry)>(at);
+    Py_RETURN_NONE;
+}
+
+// bind(addresses of the first six entry points, in their order, then current_device and current_stream, the library's version, the
 // sizes of the binding's two argument blocks, torch's version).  ImportError if this file was compiled for others: a call from here
 // hands the library pointers and strides where the header it was compiled with has them.
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -323,7 +436,7 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {METHOD(bind), METHOD(fwd), METHOD(decode), METHOD(decode_ex), METHOD(fill_fwd_ex), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {METHOD(bind), METHOD(bind_cache), METHOD(fwd), METHOD(decode), METHOD(decode_ex), METHOD(fill_fwd_ex), METHOD(norm_rope), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

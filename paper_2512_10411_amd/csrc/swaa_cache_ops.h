@@ -66,10 +66,11 @@ struct NormRopeParams {
     long long tokens;  // token slots: B Nq, or the rows of the packed tensor where the caller states them (by_row)
     int by_row;
     FastDiv div_nq;
-    // Work: a tile of 1 << tile_shift tokens times a part of the units (heads, several at once if the tile is smaller than what a
-    // workgroup takes in one go): first those of q, then k, then v.
-    int tile_shift;
+    // Work: tiles of tile_tokens tokens, 1 << wave_shift of them in a wave (its own, or with by_wave 0 the same in all four), times
+    // a part of the units (as many heads as are worked on at a time): first those of q, then k, then v.
+    int wave_shift, by_wave, tile_tokens;
     int q_units, k_units, v_units, units_per_wg, wgs_per_tile;
+    FastDiv div_wgs;  // wgs_per_tile
     long long wgs;
     float *dq_weight, *dk_weight, *partial;  // backward: results, and [wgs][2][D] sums of the workgroups
     long long tiles_per_wg;

@@ -18,6 +18,8 @@ namespace swaa {
 namespace {
 
 constexpr int kNThreads = 256;
+constexpr int kByWaveTokens = 1024;  // tokens from which on each wave has its own
+constexpr int kLeastUnits = 4;       // units that a workgroup of those has at least
 
 template <bool kF16>
 __device__ __forceinline__ void unpack(u32x4 raw, float (&x)[8]) {
@@ -68,61 +70,72 @@ __device__ __forceinline__ float row_sum(float x) {
     return x;
 }
 
-// What a workgroup knows about the tokens of its tile.
-template <int kSlots>
-struct TokenTile {
-    int pos[kSlots], b[kSlots], row[kSlots];  // row: along the tensors' row axis; b: batch entry to take strides of
-    long long k_at[kSlots], v_at[kSlots];     // where the token's key and value go, -1: nowhere
-    int live[kSlots];
+// A lane's token.
+struct Token {
+    int b, row;  // batch entry to take strides of, row along the tensors' row axis
+    int pos;
+    int of, at;  // its sequence and row in that one's cache
+    bool live;
 };
-template <int kSlots>
-__device__ __forceinline__ void find_token(const NormRopeParams &p, long long first, TokenTile<kSlots> &t) {
-    const int s = threadIdx.x;
-    if (s >> p.tile_shift) return;
-    const long long slot = first + s;
-    int b = 0, r = 0, nq = 0, nk = 0, live = slot < p.tokens;
-    int axis_row = 0;
-    if (live) {
-        if (p.by_row) {  // the sequence that holds this row of the packed tensor
-            int lo = 0, hi = p.seq.B;  // cu_q[lo] <= slot < cu_q[hi], if any holds it
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                (p.seq.cu_q[mid] <= slot ? lo : hi) = mid;
-            }
-            b = lo;
-            r = (int)(slot - p.seq.cu_q[b]);
-        } else {
-            b = (int)fastdiv((unsigned)slot, p.div_nq);
-            r = (int)(slot - (long long)b * p.seq.Nq);
+__device__ __forceinline__ Token find_token(const NormRopeParams &p, long long slot) {
+    Token t;
+    int b = 0, r = 0, nq = 0, nk = 0;
+    t.live = slot < p.tokens;
+    const int mine = (int)min(slot, p.tokens - 1);
+    if (p.by_row) {  // the sequence that holds this row of the packed tensor: as many of the others' ends as lie at or before it
+        const int lane = threadIdx.x & 63;
+        for (int c0 = 0; c0 < p.seq.B; c0 += 64) {
+            const int end = p.seq.cu_q[min(c0 + lane, p.seq.B - 1) + 1], n = min(64, p.seq.B - c0);
+            for (int i = 0; i < n; ++i) b += (int)wave_read_lane((unsigned)end, i) <= mine;
+            if ((int)wave_read_lane((unsigned)end, n - 1) > (int)wave_read_lane((unsigned)mine, 63)) break;  // (the wave's last token is found)
         }
-        sequence(p.seq, b, nq, nk);
-        live = r >= 0 && r < nq;
-        axis_row = r + (p.seq.cu_q ? p.seq.cu_q[b] : 0);
+        t.live = t.live && b < p.seq.B;
+        b = min(b, p.seq.B - 1);
+        r = mine - p.seq.cu_q[b];
+    } else {
+        b = (int)fastdiv((unsigned)mine, p.div_nq);
+        r = mine - b * p.seq.Nq;
     }
-    t.live[s] = live;
-    t.b[s] = p.seq.cu_q ? 0 : b;
-    t.row[s] = axis_row;
-    const int row = nk - nq + r;
-    t.pos[s] = !live ? 0 : !p.positions ? row : p.positions[p.seq.cu_q ? axis_row : b * (long long)p.seq.Nq + r];
-    t.k_at[s] = t.v_at[s] = -1;
-    if (live) {
-        bool inside;
-        const long long row0 = p.seq.cu_k && !p.pages.block_table ? p.seq.cu_k[b] : 0;
-        const long long k_at = cache_row(p.pages, p.k_out, b, row0, row, p.seq.cu_k != nullptr, inside);
-        if (inside) t.k_at[s] = k_at;
-        const long long v_at = cache_row(p.pages, p.v_out, b, row0, row, p.seq.cu_k != nullptr, inside);
-        if (inside) t.v_at[s] = v_at;
-    }
+    sequence(p.seq, b, nq, nk);
+    t.live = t.live && r >= 0 && r < nq;
+    t.of = b;
+    t.b = p.seq.cu_q ? 0 : b;
+    t.row = r + (p.seq.cu_q ? p.seq.cu_q[b] : 0);
+    t.at = nk - nq + r;
+    t.pos = !t.live ? 0 : !p.positions ? t.at : p.positions[p.seq.cu_q ? (long long)t.row : b * (long long)p.seq.Nq + r];
+    return t;
 }
 
-// cos and sin of the tile's tokens, [pair][token]: the angle in turns in 64 bits, what is left of it behind whole turns in 32.
-__device__ __forceinline__ void find_angles(const NormRopeParams &p, const int *pos, float2 *table) {
-    const int token = threadIdx.x & ((1 << p.tile_shift) - 1);
-    for (int pair = threadIdx.x >> p.tile_shift; pair < p.R / 2; pair += kNThreads >> p.tile_shift) {
-        const double turns = (double)pos[token] * (double)p.inv_freq[pair] * 0.15915494309189533577;
+// The place of a lane in the work: its row slot among the workgroup's, and what that is.
+template <int kLanes>
+struct Place {
+    int chunk, token;        // its 16 bytes of a row, its token of the tile
+    int head0, heads;        // of a unit's heads the one it has, and how many those are
+    int of_wave;             // its token among those in its wave, whose angles stand at `table`
+    float2 *table;
+    __device__ __forceinline__ Place(const NormRopeParams &p, float2 *lds) {
+        const int slot = (int)threadIdx.x / kLanes, of_group = p.by_wave ? slot % (64 / kLanes) : slot;
+        chunk = (int)threadIdx.x % kLanes;
+        of_wave = slot & ((1 << p.wave_shift) - 1);
+        head0 = of_group >> p.wave_shift;
+        heads = (p.by_wave ? 64 / kLanes : kNThreads / kLanes) >> p.wave_shift;
+        token = of_wave + (p.by_wave ? ((int)threadIdx.x / 64) << p.wave_shift : 0);
+        table = lds + (p.by_wave ? ((int)threadIdx.x / 64) * (p.R / 2) << p.wave_shift : 0);
+    }
+};
+
+// cos and sin of the tokens of a wave, [pair][token], by the wave for itself or by all four for their common ones: the angle in
+// turns in 64 bits, what is left of it behind whole turns in 32.  (Token i of a wave is in the lanes of its row i.)
+template <int kLanes>
+__device__ __forceinline__ void find_angles(const NormRopeParams &p, int pos, float2 *table) {
+    const int thread = p.by_wave ? (int)threadIdx.x % 64 : (int)threadIdx.x, threads = p.by_wave ? 64 : kNThreads;
+    const int token = thread & ((1 << p.wave_shift) - 1);
+    const double at = (double)__shfl(pos, token * kLanes);
+    for (int pair = thread >> p.wave_shift; pair < p.R / 2; pair += threads >> p.wave_shift) {
+        const double turns = at * (double)p.inv_freq[pair] * 0.15915494309189533577;
         float s, c;
         sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-        table[(pair << p.tile_shift) + token] = make_float2(c, s);
+        table[(pair << p.wave_shift) + token] = make_float2(c, s);
     }
 }
 
@@ -130,11 +143,13 @@ __device__ __forceinline__ void find_angles(const NormRopeParams &p, const int *
 struct Turn {
     float c[8], s[8];  // y_j = n_j c_j + n_partner s_j
     int partner;       // lane that holds the partners (pairs of halves)
+    bool swap;         // (the lanes of a row of 16 and its halves: by an operand of a vector instruction instead of the LDS crossbar)
 };
 __device__ __forceinline__ Turn lane_turn(const NormRopeParams &p, const float2 *table, int token, int chunk) {
     Turn t;
     const int half = p.R / 16;  // chunks of half the rotated elements
     t.partner = threadIdx.x & 63;
+    t.swap = p.R == 128 && p.D == 128;
     if (8 * chunk >= p.R) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -146,7 +161,7 @@ __device__ __forceinline__ Turn lane_turn(const NormRopeParams &p, const float2 
     if (p.interleaved) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float2 cs = table[((4 * chunk + j / 2) << p.tile_shift) + token];
+            const float2 cs = table[((4 * chunk + j / 2) << p.wave_shift) + token];
             t.c[j] = cs.x;
             t.s[j] = j % 2 ? cs.y : -cs.y;
         }
@@ -156,7 +171,7 @@ __device__ __forceinline__ Turn lane_turn(const NormRopeParams &p, const float2 
     t.partner += second ? -half : half;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float2 cs = table[((8 * (second ? chunk - half : chunk) + j) << p.tile_shift) + token];
+        const float2 cs = table[((8 * (second ? chunk - half : chunk) + j) << p.wave_shift) + token];
         t.c[j] = cs.x;
         t.s[j] = second ? cs.y : -cs.y;
     }
@@ -168,6 +183,9 @@ __device__ __forceinline__ u32x4 partners(u32x4 raw, const Turn &t, bool interle
     if (interleaved) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) r[j] = (raw[j] >> 16) | (raw[j] << 16);
+    } else if (t.swap) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = (unsigned)__builtin_amdgcn_update_dpp(0, (int)raw[j], 0x128, 0xf, 0xf, true);  // row_ror:8
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) r[j] = (unsigned)__shfl((int)raw[j], t.partner);
@@ -187,141 +205,168 @@ __device__ __forceinline__ void partner_weights(const float *w, const NormRopePa
     for (int j = 0; j < 8; ++j) out[j] = w && turns ? w[base + (p.interleaved ? j ^ 1 : j)] : 1.f;
 }
 
+// A lane's way through the heads of one tensor, from unit `unit` on: the head of unit u exists while u < end.
+struct Heads {
+    char *at;
+    long long step;  // bytes from unit to unit
+    int end;
+    __device__ __forceinline__ Heads(const Rows &t, long long offset, int H, int head0, int heads, int first, int unit, bool live) {
+        at = t.ptr + 2 * (offset + (head0 + (long long)(unit > first ? unit - first : 0) * heads) * t.sh);
+        step = 2 * (long long)heads * t.sh;
+        end = live ? first + (H - head0 + heads - 1) / heads : 0;
+    }
+};
+
 constexpr int kAhead = 4;  // rows of a lane on the way at a time
 
 template <int kLanes, bool kF16>
-__global__ __launch_bounds__(kNThreads) void swaa_norm_rope_kernel(const NormRopeParams p) {
-    constexpr int kSlots = kNThreads / kLanes;
-    __shared__ TokenTile<kSlots> tile;
+__global__ __launch_bounds__(kNThreads, 4) void swaa_norm_rope_kernel(const NormRopeParams p) {
+    fetch_args<NormRopeParams>();
     extern __shared__ float2 table[];
-    const int tid = threadIdx.x;
-    const unsigned of_tile = blockIdx.x / (unsigned)p.wgs_per_tile, part = blockIdx.x - of_tile * (unsigned)p.wgs_per_tile;
-    find_token<kSlots>(p, (long long)of_tile << p.tile_shift, tile);
-    __syncthreads();
-    find_angles(p, tile.pos, table);
-    __syncthreads();
-
-    const int chunk = tid % kLanes, slot = tid / kLanes;
-    const int token = slot & ((1 << p.tile_shift) - 1), head0 = slot >> p.tile_shift;
-    const int heads = kSlots >> p.tile_shift;  // at a time
-    const bool in_row = 8 * chunk < p.D, live = tile.live[token] && in_row;
-    const long long b = tile.b[token], row = tile.row[token];
-    const Turn turn = lane_turn(p, table, token, chunk);
-
-    int u = (int)part * p.units_per_wg;
-    const int u_end = min(u + p.units_per_wg, p.q_units + p.k_units + p.v_units);
-    const float inv_d = 1.f / (float)p.D;
-    // units [u, of_part end) of one of q, k, v
-    auto pass = [&](const Rows &in, const Rows &out, long long out_at, int H, int first, int units, const float *w, bool plain) {
-        const int end = min(u_end, first + units);
-        if (u >= end) return;
-        float a[8], bq[8];
-        if (!plain) {
-            float wj[8], wp[8];
-            row_weights(w, chunk, in_row, wj);
-            partner_weights(w, p, chunk, wp);
+    const unsigned of_tile = fastdiv(blockIdx.x, p.div_wgs), part = blockIdx.x - of_tile * (unsigned)p.wgs_per_tile;
+    const Place<kLanes> at(p, table);
+    const int chunk = at.chunk;
+    const bool in_row = 8 * chunk < p.D;
+    const Token t = find_token(p, (long long)of_tile * p.tile_tokens + at.token);
+    const bool live = t.live && in_row;
+    const int k_first = p.q_units, v_first = k_first + p.k_units;
+    const int u_begin = (int)part * p.units_per_wg, u_end = min(u_begin + p.units_per_wg, v_first + p.v_units);
+    auto heads_of = [&](const Rows &x, long long offset, int H, int first, bool there) {
+        return Heads(x, offset + 8 * chunk, H, at.head0, at.heads, first, u_begin, there);
+    };
+    // kinds of rows one behind the other: what is true of the one that unit u has
+    auto load = [&](Heads &from, int u, int end, u32x4 (&raw)[kAhead]) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                a[j] = wj[j] * turn.c[j];
-                bq[j] = wp[j] * turn.s[j];
-            }
+        for (int i = 0; i < kAhead; ++i) {
+            raw[i] = u32x4{0, 0, 0, 0};
+            if (u + i < end && u + i < from.end) raw[i] = *reinterpret_cast<const u32x4 *>(from.at);
+            from.at += from.step;
         }
-        const char *src = in.ptr + 2 * (b * in.sb + row * in.sn + 8 * chunk);
-        char *dst = out.ptr + 2 * (out_at + 8 * chunk);
-        for (; u < end; u += kAhead) {
-            u32x4 raw[kAhead];
+    };
+    Heads q_in = heads_of(p.q, t.b * p.q.sb + t.row * p.q.sn, p.Hq, 0, live);
+    Heads k_in = heads_of(p.k, t.b * p.k.sb + t.row * p.k.sn, p.Hkv, k_first, live);
+    u32x4 raw[kAhead];
+    const int q_end = min(u_end, k_first), k_begin = max(u_begin, k_first), k_end = min(u_end, v_first), v_begin = max(u_begin, v_first);
+    if (u_begin < q_end)  // (the first rows are on the way while the angles are worked out)
+        load(q_in, u_begin, q_end, raw);
+    else if (k_begin < k_end)
+        load(k_in, k_begin, k_end, raw);
+
+    const float inv_d = 1.f / (float)p.D;
+    Turn turn;
+    if (u_begin < v_first) {
+        find_angles<kLanes>(p, t.pos, at.table);
+        __syncthreads();
+        turn = lane_turn(p, at.table, at.of_wave, chunk);
+    }
+    auto rows = [&](Heads &from, Heads &to, int begin, int end, const float *w) {
+        float a[8], b[8];  // weight times cosine, the partner's times sine
+        row_weights(w, chunk, in_row, a);
+        partner_weights(w, p, chunk, b);
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int h = (u + i - first) * heads + head0;
-                raw[i] = u32x4{0, 0, 0, 0};
-                if (u + i < end && h < H && live) raw[i] = *reinterpret_cast<const u32x4 *>(src + 2 * (h * in.sh));
-            }
+        for (int j = 0; j < 8; ++j) {
+            a[j] *= turn.c[j];
+            b[j] *= turn.s[j];
+        }
+        for (int u = begin; u < end; u += kAhead) {
+            if (u > u_begin) load(from, u, end, raw);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 if (u + i >= end) break;
-                const int h = (u + i - first) * heads + head0;
-                if (!plain) {
-                    float x[8], xp[8], y[8];
-                    unpack<kF16>(raw[i], x);
-                    unpack<kF16>(partners(raw[i], turn, p.interleaved), xp);
-                    float r = 1.f;
-                    if (w) {
-                        float ss = 0.f;
+                float x[8], xp[8], y[8];
+                unpack<kF16>(raw[i], x);
+                unpack<kF16>(partners(raw[i], turn, p.interleaved), xp);
+                float r = 1.f;
+                if (w) {
+                    float ss = 0.f;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) ss += x[j] * x[j];
-                        r = 1.f / sqrtf(row_sum<kLanes>(ss) * inv_d + p.eps);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y[j] = r * (x[j] * a[j] + xp[j] * bq[j]);
-                    raw[i] = pack<kF16>(y);
+                    for (int j = 0; j < 8; ++j) ss += x[j] * x[j];
+                    r = __builtin_amdgcn_rsqf(row_sum<kLanes>(ss) * inv_d + p.eps);
                 }
-                if (h < H && live && out_at >= 0) *reinterpret_cast<u32x4 *>(dst + 2 * (h * out.sh)) = raw[i];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = r * (x[j] * a[j] + xp[j] * b[j]);
+                if (u + i < to.end) *reinterpret_cast<u32x4 *>(to.at) = pack<kF16>(y);
+                to.at += to.step;
             }
         }
-        u = end;
     };
-    pass(p.q, p.q_out, b * p.q_out.sb + row * p.q_out.sn, p.Hq, 0, p.q_units, p.q_weight, false);
-    pass(p.k, p.k_out, tile.k_at[token], p.Hkv, p.q_units, p.k_units, p.k_weight, false);
-    pass(p.v, p.v_out, tile.v_at[token], p.Hkv, p.q_units + p.k_units, p.v_units, nullptr, true);
+    if (u_begin < q_end) {
+        Heads q_out = heads_of(p.q_out, t.b * p.q_out.sb + t.row * p.q_out.sn, p.Hq, 0, live);
+        rows(q_in, q_out, u_begin, q_end, p.q_weight);
+    }
+    if (u_end <= k_first) return;
+    const long long row0 = p.seq.cu_k && !p.pages.block_table ? p.seq.cu_k[t.of] : 0;
+    const int row = t.live ? t.at : 0;
+    bool inside;
+    if (k_begin < k_end) {
+        const long long k_at = cache_row(p.pages, p.k_out, t.of, row0, row, p.seq.cu_k != nullptr, inside);
+        Heads k_out = heads_of(p.k_out, k_at, p.Hkv, k_first, live && inside);
+        rows(k_in, k_out, k_begin, k_end, p.k_weight);
+    }
+    if (v_begin >= u_end) return;
+    const long long v_at = cache_row(p.pages, p.v_out, t.of, row0, row, p.seq.cu_k != nullptr, inside);
+    Heads v_in = heads_of(p.v, t.b * p.v.sb + t.row * p.v.sn, p.Hkv, v_first, live), v_out = heads_of(p.v_out, v_at, p.Hkv, v_first, live && inside);
+    for (int u = v_begin; u < u_end; u += kAhead) {
+        load(v_in, u, u_end, raw);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (u + i < u_end && u + i < v_out.end) *reinterpret_cast<u32x4 *>(v_out.at) = raw[i];
+            v_out.at += v_out.step;
+        }
+    }
 }
 
+constexpr int kBwdAhead = 2;
+
 template <int kLanes, bool kF16>
-__global__ __launch_bounds__(kNThreads) void swaa_norm_rope_bwd_kernel(const NormRopeParams p) {
-    constexpr int kSlots = kNThreads / kLanes;
-    constexpr int kBwdAhead = 2;
-    __shared__ TokenTile<kSlots> tile;
+__global__ __launch_bounds__(kNThreads, 4) void swaa_norm_rope_bwd_kernel(const NormRopeParams p) {
+    fetch_args<NormRopeParams>();
     __shared__ float sums[4][2][kLanes * 8];
     extern __shared__ float2 table[];
     const int tid = threadIdx.x;
-    const unsigned group = blockIdx.x / (unsigned)p.wgs_per_tile, part = blockIdx.x - group * (unsigned)p.wgs_per_tile;
-    const int chunk = tid % kLanes, slot = tid / kLanes;
-    const int token = slot & ((1 << p.tile_shift) - 1), head0 = slot >> p.tile_shift;
-    const int heads = kSlots >> p.tile_shift;
+    const unsigned group = fastdiv(blockIdx.x, p.div_wgs), part = blockIdx.x - group * (unsigned)p.wgs_per_tile;
+    const Place<kLanes> at(p, table);
+    const int chunk = at.chunk;
     const bool in_row = 8 * chunk < p.D;
     const float inv_d = 1.f / (float)p.D;
+    const int k_first = p.q_units, u_begin = (int)part * p.units_per_wg, u_end = min(u_begin + p.units_per_wg, k_first + p.k_units);
     float dw[2][8];  // of q and of k
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[0][j] = dw[1][j] = 0.f;
 
     for (long long n = 0; n < p.tiles_per_wg; ++n) {
-        const long long first = ((long long)group * p.tiles_per_wg + n) << p.tile_shift;
-        if (first >= p.tokens) break;
-        __syncthreads();  // (the tile before is done with)
-        find_token<kSlots>(p, first, tile);
+        const long long first_token = ((long long)group * p.tiles_per_wg + n) * p.tile_tokens;
+        if (first_token >= p.tokens) break;
+        const Token t = find_token(p, first_token + at.token);
+        const bool live = t.live && in_row;
+        if (n > 0) __syncthreads();  // (the tile before's angles are done with)
+        find_angles<kLanes>(p, t.pos, at.table);
         __syncthreads();
-        find_angles(p, tile.pos, table);
-        __syncthreads();
-        const bool live = tile.live[token] && in_row;
-        const long long b = tile.b[token], row = tile.row[token];
-        const Turn turn = lane_turn(p, table, token, chunk);
-        int u = (int)part * p.units_per_wg;
-        const int u_end = min(u + p.units_per_wg, p.q_units + p.k_units);
-        auto pass = [&](const Rows &in, const Rows &grad, const Rows &out, int H, int first_unit, int units, const float *w, float (&sum)[8]) {
-            const int end = min(u_end, first_unit + units);
-            if (u >= end) return;
+        const Turn turn = lane_turn(p, at.table, at.of_wave, chunk);
+        auto rows = [&](const Rows &x_of, const Rows &dy_of, const Rows &dx_of, int H, int first, int begin, int end, const float *w, float (&sum)[8]) {
+            if (begin >= end) return;
+            auto heads_of = [&](const Rows &r) { return Heads(r, t.b * r.sb + t.row * r.sn + 8 * chunk, H, at.head0, at.heads, first, begin, live); };
+            Heads x_in = heads_of(x_of), dy = heads_of(dy_of), dx = heads_of(dx_of);
             float wj[8];
             row_weights(w, chunk, in_row, wj);
-            const char *src = in.ptr + 2 * (b * in.sb + row * in.sn + 8 * chunk);
-            const char *gsrc = grad.ptr + 2 * (b * grad.sb + row * grad.sn + 8 * chunk);
-            char *dst = out.ptr + 2 * (b * out.sb + row * out.sn + 8 * chunk);
-            for (; u < end; u += kBwdAhead) {
-                u32x4 raw[kBwdAhead], graw[kBwdAhead];
+            for (int u = begin; u < end; u += kBwdAhead) {
+                u32x4 raw[kBwdAhead], grad[kBwdAhead];
 #pragma unroll
                 for (int i = 0; i < kBwdAhead; ++i) {
-                    const int h = (u + i - first_unit) * heads + head0;
-                    raw[i] = graw[i] = u32x4{0, 0, 0, 0};
-                    if (u + i < end && h < H && live) {
-                        graw[i] = *reinterpret_cast<const u32x4 *>(gsrc + 2 * (h * grad.sh));
-                        if (w) raw[i] = *reinterpret_cast<const u32x4 *>(src + 2 * (h * in.sh));
+                    raw[i] = grad[i] = u32x4{0, 0, 0, 0};
+                    if (u + i < end && u + i < dy.end) {
+                        grad[i] = *reinterpret_cast<const u32x4 *>(dy.at);
+                        if (w) raw[i] = *reinterpret_cast<const u32x4 *>(x_in.at);
                     }
+                    dy.at += dy.step;
+                    x_in.at += x_in.step;
                 }
 #pragma unroll
                 for (int i = 0; i < kBwdAhead; ++i) {
                     if (u + i >= end) break;
-                    const int h = (u + i - first_unit) * heads + head0;
                     float g[8], gp[8];
-                    unpack<kF16>(graw[i], g);
-                    unpack<kF16>(partners(graw[i], turn, p.interleaved), gp);
+                    unpack<kF16>(grad[i], g);
+                    unpack<kF16>(partners(grad[i], turn, p.interleaved), gp);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) g[j] = g[j] * turn.c[j] - gp[j] * turn.s[j];
                     if (w) {
@@ -332,7 +377,7 @@ __global__ __launch_bounds__(kNThreads) void swaa_norm_rope_bwd_kernel(const Nor
                             ss += x[j] * x[j];
                             dot += x[j] * wj[j] * g[j];
                         }
-                        const float r = 1.f / sqrtf(row_sum<kLanes>(ss) * inv_d + p.eps);
+                        const float r = __builtin_amdgcn_rsqf(row_sum<kLanes>(ss) * inv_d + p.eps);
                         const float along = row_sum<kLanes>(dot) * inv_d * r * r;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
@@ -340,66 +385,74 @@ __global__ __launch_bounds__(kNThreads) void swaa_norm_rope_bwd_kernel(const Nor
                             g[j] = r * (wj[j] * g[j] - x[j] * along);
                         }
                     }
-                    if (h < H && live) *reinterpret_cast<u32x4 *>(dst + 2 * (h * out.sh)) = pack<kF16>(g);
+                    if (u + i < dx.end) *reinterpret_cast<u32x4 *>(dx.at) = pack<kF16>(g);
+                    dx.at += dx.step;
                 }
             }
-            u = end;
         };
-        pass(p.q, p.dq_out, p.q_out, p.Hq, 0, p.q_units, p.q_weight, dw[0]);
-        pass(p.k, p.dk_out, p.k_out, p.Hkv, p.q_units, p.k_units, p.k_weight, dw[1]);
+        rows(p.q, p.dq_out, p.q_out, p.Hq, 0, u_begin, min(u_end, k_first), p.q_weight, dw[0]);
+        rows(p.k, p.dk_out, p.k_out, p.Hkv, k_first, max(u_begin, k_first), u_end, p.k_weight, dw[1]);
     }
     if (!p.partial) return;
     // lanes of the same place in a row, then the four waves
 #pragma unroll
-    for (int part_of = 0; part_of < 2; ++part_of)
+    for (int of_k = 0; of_k < 2; ++of_k)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float x = dw[part_of][j];
+            float x = dw[of_k][j];
 #pragma unroll
             for (int d = kLanes; d < 64; d *= 2) x += __shfl_xor(x, d);
-            if ((tid & 63) < kLanes) sums[tid / 64][part_of][8 * chunk + j] = x;
+            if ((tid & 63) < kLanes) sums[tid / 64][of_k][8 * chunk + j] = x;
         }
     __syncthreads();
     for (int i = tid; i < 2 * p.D; i += kNThreads) {
-        const int part_of = i >= p.D, d = i - part_of * p.D;
-        p.partial[(long long)blockIdx.x * 2 * p.D + i] =
-            (sums[0][part_of][d] + sums[1][part_of][d]) + (sums[2][part_of][d] + sums[3][part_of][d]);
+        const int of_k = i >= p.D, d = i - of_k * p.D;
+        p.partial[(long long)blockIdx.x * 2 * p.D + i] = (sums[0][of_k][d] + sums[1][of_k][d]) + (sums[2][of_k][d] + sums[3][of_k][d]);
     }
 }
 
-// The workgroups' sums added up, always in the same order: 16 columns a workgroup, 16 lanes to each.
-__global__ __launch_bounds__(kNThreads) void swaa_norm_weight_sums_kernel(const float *partial, long long n, int D, float *dq_weight, float *dk_weight) {
-    __shared__ float sums[16][17];
-    const int col = blockIdx.x * 16 + threadIdx.x % 16, lane = threadIdx.x / 16;
+// The workgroups' sums added up, always in the same order: 16 columns a workgroup, 64 lanes to each.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void swaa_norm_weight_sums_kernel(const float *partial, long long n, int D, float *dq_weight, float *dk_weight) {
+    __shared__ float sums[64][17];
+    const int col = blockIdx.x * 16 + threadIdx.x % 16, lane = threadIdx.x / 16;  // (2 D is a multiple of 16)
     float x = 0.f;
-    if (col < 2 * D)
-        for (long long i = lane; i < n; i += 16) x += partial[i * 2 * D + col];
+#pragma unroll 8
+    for (long long i = lane; i < n; i += 64) x += partial[i * 2 * D + col];
     sums[lane][threadIdx.x % 16] = x;
     __syncthreads();
-    if (threadIdx.x < 16 && col < 2 * D) {
-        float all = 0.f;
-        for (int i = 0; i < 16; ++i) all += sums[i][threadIdx.x];
-        (col < D ? dq_weight : dk_weight)[col < D ? col : col - D] = all;
+    if (threadIdx.x < 64) {
+        float part = 0.f;  // four threads to a column
+        for (int i = 0; i < 16; ++i) part += sums[16 * (threadIdx.x / 16) + i][threadIdx.x % 16];
+        part += __shfl_xor(part, 16);
+        part += __shfl_xor(part, 32);
+        if (threadIdx.x < 16) (col < D ? dq_weight : dk_weight)[col < D ? col : col - D] = part;
     }
 }
 
 int lanes_of_row(int D) { return D <= 32 ? 4 : D <= 64 ? 8 : D <= 128 ? 16 : 32; }
 
-// Tile and units: a tile of as many tokens as a workgroup takes rows at a time, fewer if there are fewer; the units of a tile are
-// shared out over workgroups until there are `target`.
+// Tile and units.  A wave has as many tokens as rows at a time (four of head dimension 128), fewer if there are fewer.  Few tokens: the
+// four waves share them and take different heads.  Many: each wave has its own and goes through the heads by itself.  The
+// units of a tile are shared out over workgroups until there are `target`.
 bool plan(NormRopeParams &p, int target, bool backward) {
-    const int slots = kNThreads / lanes_of_row(p.D);
-    p.tile_shift = 0;
-    while ((2 << p.tile_shift) <= slots && (1LL << p.tile_shift) < p.tokens) ++p.tile_shift;
-    const int heads = slots >> p.tile_shift;
+    const int wave_rows = 64 / lanes_of_row(p.D);
+    p.wave_shift = 0;
+    while ((2 << p.wave_shift) <= wave_rows && (1LL << p.wave_shift) < p.tokens) ++p.wave_shift;
+    p.by_wave = p.tokens >= kByWaveTokens ? 1 : 0;
+    p.tile_tokens = (p.by_wave ? 4 : 1) << p.wave_shift;
+    const int heads = (p.by_wave ? wave_rows : 4 * wave_rows) >> p.wave_shift;
     p.q_units = (p.Hq + heads - 1) / heads;
     p.k_units = (p.Hkv + heads - 1) / heads;
     p.v_units = p.v.ptr ? p.k_units : 0;
     const int units = p.q_units + p.k_units + p.v_units;
-    const long long tiles = (p.tokens + (1LL << p.tile_shift) - 1) >> p.tile_shift;
+    const long long tiles = (p.tokens + p.tile_tokens - 1) / p.tile_tokens;
     const long long parts = tiles >= target ? 1 : (target + tiles - 1) / tiles;
     p.units_per_wg = (int)((units + parts - 1) / parts);
+    const int least = p.by_wave ? kLeastUnits : 1;
+    if (p.units_per_wg < least) p.units_per_wg = least < units ? least : units;
     p.wgs_per_tile = (units + p.units_per_wg - 1) / p.units_per_wg;
+    p.div_wgs = make_fastdiv((unsigned)p.wgs_per_tile);
     p.tiles_per_wg = backward ? (tiles + target - 1) / target : 1;
     p.wgs = (tiles + p.tiles_per_wg - 1) / p.tiles_per_wg * p.wgs_per_tile;
     return p.wgs <= 0x7fffffffLL;
@@ -407,7 +460,7 @@ bool plan(NormRopeParams &p, int target, bool backward) {
 
 template <template <int, bool> class Kernel>
 hipError_t dispatch(const NormRopeParams &p, hipStream_t stream) {
-    const size_t lds = sizeof(float2) * (size_t)(p.R / 2) << p.tile_shift;
+    const size_t lds = sizeof(float2) * (size_t)(p.R / 2) * p.tile_tokens;
     auto go = [&](auto kernel) {
         kernel<<<dim3((unsigned)p.wgs), dim3(kNThreads), lds, stream>>>(p);
         return hipGetLastError();
@@ -430,7 +483,7 @@ struct Bwd {
 
 }  // namespace
 
-bool plan_norm_rope(NormRopeParams &p) { return plan(p, 2048, false); }
+bool plan_norm_rope(NormRopeParams &p) { return plan(p, 1024, false); }
 bool plan_norm_rope_bwd(NormRopeParams &p) { return plan(p, 1024, true); }
 
 hipError_t launch_norm_rope(const NormRopeParams &p, hipStream_t stream) { return dispatch<Fwd>(p, stream); }
@@ -438,7 +491,7 @@ hipError_t launch_norm_rope(const NormRopeParams &p, hipStream_t stream) { retur
 hipError_t launch_norm_rope_bwd(const NormRopeParams &p, hipStream_t stream) {
     const hipError_t err = dispatch<Bwd>(p, stream);
     if (err != hipSuccess || !p.partial) return err;
-    swaa_norm_weight_sums_kernel<<<dim3((2 * p.D + 15) / 16), dim3(kNThreads), 0, stream>>>(p.partial, p.wgs, p.D, p.dq_weight, p.dk_weight);
+    swaa_norm_weight_sums_kernel<<<dim3(2 * p.D / 16), dim3(kSumThreads), 0, stream>>>(p.partial, p.wgs, p.D, p.dq_weight, p.dk_weight);
     return hipGetLastError();
 }
 
