@@ -229,7 +229,7 @@ class _NoHostCalls:
     def fwd(*args):
         return None
 
-    decode = decode_ex = fill_fwd_ex = norm_rope = fwd
+    decode = decode_ex = fill_fwd_ex = norm_rope = norm_rope_bwd = fwd
 
 
 def _native_part(torch):
@@ -244,7 +244,9 @@ def _native_part(torch):
             lib.swaa_attn_decode_ex, lib.swaa_attn_decode_ex_workspace_bytes)),
             torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
             lib.swaa_version(), ctypes.sizeof(SwaaFwdArgs), ctypes.sizeof(SwaaDecodeArgs), str(torch.__version__))
-        _host_calls.bind_cache(ctypes.cast(lib.swaa_qk_norm_rope, ctypes.c_void_p).value, ctypes.sizeof(SwaaNormRopeArgs))
+        _host_calls.bind_cache(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            lib.swaa_qk_norm_rope, lib.swaa_qk_norm_rope_bwd, lib.swaa_qk_norm_rope_bwd_workspace_bytes)),
+            ctypes.sizeof(SwaaNormRopeArgs), ctypes.sizeof(SwaaNormRopeBwdArgs))
     except (ImportError, TypeError, AttributeError) as e:  # (TypeError: its `bind` takes other arguments; AttributeError: it lacks one)
         warnings.warn(f"{HOST_CALLS_PATH} is not used, calls take longer on the way to the library ({e}): "
                       "build it with `python -m paper_2512_10411_amd.build`", RuntimeWarning, stacklevel=4)
@@ -1013,6 +1015,10 @@ def swaa_qk_norm_rope_bwd(dq_out, dk_out, q, k, inv_freq=None, positions=None, q
     workspace: a uint8 tensor of swaa_qk_norm_rope_bwd_workspace_bytes(...) bytes (allocated here with torch when None).
     """
     tc = torch or _torch()
+    if dq is None and dk is None and workspace is None and stream is None:
+        r = _host.norm_rope_bwd(dq_out, dk_out, q, k, inv_freq, positions, q_weight, k_weight, eps, interleaved)
+        if r is not None:
+            return _results(r)
     _elements(tc, q, "q")
     _elements(tc, k, "k", q)
     for name, t, like in (("dq_out", dq_out, q), ("dk_out", dk_out, k), ("dq", dq, q), ("dk", dk, k)):

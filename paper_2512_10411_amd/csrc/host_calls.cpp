@@ -285,6 +285,8 @@ PyObject *fill_fwd_ex(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 decltype(&swaa_qk_norm_rope) norm_rope_entry;
+decltype(&swaa_qk_norm_rope_bwd) norm_rope_bwd_entry;
+decltype(&swaa_qk_norm_rope_bwd_workspace_bytes) norm_rope_bwd_workspace_entry;
 
 // swaa_tensor of a view [blocks, heads, rows, D] or [heads, rows, D] (a dimension of one entry has no stride to speak of).
 swaa_tensor rows_of(const at::Tensor &t) {
@@ -380,20 +382,85 @@ PyObject *norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// bind_cache(address of the entry point above, size of the binding's argument block), behind bind, which has checked the library.
+// norm_rope_bwd(dq_out, dk_out, q, k, inv_freq, positions, q_weight, k_weight, eps, interleaved): (dq, dk, dq_weight, dk_weight)
+PyObject *norm_rope_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int device;
+    swaa_norm_rope_bwd_args s{};
+    if (n != 10 || !plain_call(a[2], device, s.stream)) Py_RETURN_NONE;
+    const at::Tensor *x[4], *t;  // dq_out, dk_out, q, k
+    for (int i = 0; i < 4; ++i) {
+        x[i] = plain_tensor(a[i], device);
+        if (!x[i] || x[i]->dim() != 4 || x[i]->stride(3) != 1) Py_RETURN_NONE;
+    }
+    const at::Tensor &q = *x[2], &k = *x[3];
+    if (q.scalar_type() != at::kBFloat16 && q.scalar_type() != at::kHalf) Py_RETURN_NONE;
+    for (const at::Tensor *y : x)
+        if (y->scalar_type() != q.scalar_type()) Py_RETURN_NONE;
+    const int64_t B = q.size(0), N = q.size(2), D = q.size(3);
+    if (k.size(0) != B || k.size(2) != N || k.size(3) != D || x[0]->sizes() != q.sizes() || x[1]->sizes() != k.sizes()) Py_RETURN_NONE;
+    s.B = (int)B, s.Hq = (int)q.size(1), s.Hkv = (int)k.size(1), s.D = (int)D, s.N = (int)N;
+    if (a[4] != Py_None) {
+        t = plain_tensor(a[4], device);
+        if (!t || t->scalar_type() != at::kFloat || !t->is_contiguous()) Py_RETURN_NONE;
+        s.inv_freq = static_cast<const float *>(t->data_ptr()), s.rot_dim = (int)(2 * t->numel());
+    }
+    if (!plain_numbers(a[5], device, at::kInt, {B, N}, s.positions)) Py_RETURN_NONE;
+    const bool norm = a[6] != Py_None;
+    if (norm != (a[7] != Py_None) || !plain_numbers(a[6], device, at::kFloat, {D}, s.q_weight) || !plain_numbers(a[7], device, at::kFloat, {D}, s.k_weight))
+        Py_RETURN_NONE;
+    if (!PyFloat_CheckExact(a[8]) || !PyBool_Check(a[9])) Py_RETURN_NONE;
+    s.eps = (float)PyFloat_AS_DOUBLE(a[8]), s.interleaved = a[9] == Py_True;
+    s.dtype = q.scalar_type() == at::kHalf ? SWAA_F16 : SWAA_BF16;
+    const long long need = norm_rope_bwd_workspace_entry(&s);
+    if (need < 0) return PyLong_FromLongLong(need);
+    const at::Tensor dq = at::empty_like(q), dk = at::empty_like(k);
+    at::Tensor workspace, dw[2];
+    if (need > 0) workspace = empty_bytes(q, need), s.workspace = workspace.data_ptr(), s.workspace_bytes = need;
+    if (norm) {
+        for (at::Tensor &w : dw) w = empty_floats(q, {D});
+        s.dq_weight = static_cast<float *>(dw[0].data_ptr()), s.dk_weight = static_cast<float *>(dw[1].data_ptr());
+    }
+    s.dq_out = rows_of(*x[0]), s.dk_out = rows_of(*x[1]), s.q = rows_of(q), s.k = rows_of(k), s.dq = rows_of(dq), s.dk = rows_of(dk);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = norm_rope_bwd_entry(&s);
+    Py_END_ALLOW_THREADS
+    if (rc != SWAA_OK) return PyLong_FromLong(rc);
+    PyObject *all = PyTuple_New(4);
+    if (!all) return nullptr;
+    PyTuple_SET_ITEM(all, 0, THPVariable_Wrap(dq));
+    PyTuple_SET_ITEM(all, 1, THPVariable_Wrap(dk));
+    for (int i = 0; i < 2; ++i) {
+        if (!norm) Py_INCREF(Py_None);
+        PyTuple_SET_ITEM(all, 2 + i, norm ? THPVariable_Wrap(dw[i]) : Py_None);
+    }
+    return all;
+    END_HANDLE_TH_ERRORS
+}
+
+// bind_cache(addresses of the three entry points above, sizes of the binding's two argument blocks), behind bind, which has checked
+// the library.
 PyObject *bind_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    if (n != 2) {
-        PyErr_SetString(PyExc_TypeError, "bind_cache takes an address and a number");
+    if (n != 5) {
+        PyErr_SetString(PyExc_TypeError, "bind_cache takes three addresses and two numbers");
         return nullptr;
     }
-    void *at = PyLong_AsVoidPtr(a[0]);
-    const long long bytes = PyErr_Occurred() ? -1 : PyLong_AsLongLong(a[1]);
+    void *at[3];
+    for (int i = 0; i < 3; ++i) {
+        at[i] = PyLong_AsVoidPtr(a[i]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    const long long fwd_bytes = PyLong_AsLongLong(a[3]), bwd_bytes = PyLong_AsLongLong(a[4]);
     if (PyErr_Occurred()) return nullptr;
-    if (bytes != (long long)sizeof(swaa_norm_rope_args)) {
-        PyErr_Format(PyExc_ImportError, "compiled for an argument block of %zu bytes, not %lld", sizeof(swaa_norm_rope_args), bytes);
+    if (fwd_bytes != (long long)sizeof(swaa_norm_rope_args) || bwd_bytes != (long long)sizeof(swaa_norm_rope_bwd_args)) {
+        PyErr_Format(PyExc_ImportError, "compiled for argument blocks of %zu and %zu bytes, not %lld and %lld", sizeof(swaa_norm_rope_args),
+                     sizeof(swaa_norm_rope_bwd_args), fwd_bytes, bwd_bytes);
         return nullptr;
     }
-    norm_rope_entry = reinterpret_cast<decltype(norm_rope_entry)>(at);
+    norm_rope_entry = reinterpret_cast<decltype(norm_rope_entry)>(at[0]);
+    norm_rope_bwd_entry = reinterpret_cast<decltype(norm_rope_bwd_entry)>(at[1]);
+    norm_rope_bwd_workspace_entry = reinterpret_cast<decltype(norm_rope_bwd_workspace_entry)>(at[2]);
     Py_RETURN_NONE;
 }
 
@@ -436,7 +503,7 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {METHOD(bind), METHOD(bind_cache), METHOD(fwd), METHOD(decode), METHOD(decode_ex), METHOD(fill_fwd_ex), METHOD(norm_rope), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {METHOD(bind), METHOD(bind_cache), METHOD(fwd), METHOD(decode), METHOD(decode_ex), METHOD(fill_fwd_ex), METHOD(norm_rope), METHOD(norm_rope_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
