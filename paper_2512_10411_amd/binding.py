@@ -229,7 +229,7 @@ class _NoHostCalls:
     def fwd(*args):
         return None
 
-    decode = decode_ex = fill_fwd_ex = norm_rope = norm_rope_bwd = fwd
+    decode = decode_ex = fill_fwd_ex = norm_rope = norm_rope_bwd = key_weights = evict = fwd
 
 
 def _native_part(torch):
@@ -245,8 +245,9 @@ def _native_part(torch):
             torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
             lib.swaa_version(), ctypes.sizeof(SwaaFwdArgs), ctypes.sizeof(SwaaDecodeArgs), str(torch.__version__))
         _host_calls.bind_cache(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-            lib.swaa_qk_norm_rope, lib.swaa_qk_norm_rope_bwd, lib.swaa_qk_norm_rope_bwd_workspace_bytes)),
-            ctypes.sizeof(SwaaNormRopeArgs), ctypes.sizeof(SwaaNormRopeBwdArgs))
+            lib.swaa_qk_norm_rope, lib.swaa_qk_norm_rope_bwd, lib.swaa_qk_norm_rope_bwd_workspace_bytes,
+            lib.swaa_attn_key_weights, lib.swaa_attn_key_weights_workspace_bytes, lib.swaa_cache_evict)),
+            *(ctypes.sizeof(block) for block in (SwaaNormRopeArgs, SwaaNormRopeBwdArgs, SwaaKeyWeightsArgs, SwaaEvictArgs)))
     except (ImportError, TypeError, AttributeError) as e:  # (TypeError: its `bind` takes other arguments; AttributeError: it lacks one)
         warnings.warn(f"{HOST_CALLS_PATH} is not used, calls take longer on the way to the library ({e}): "
                       "build it with `python -m paper_2512_10411_amd.build`", RuntimeWarning, stacklevel=4)
@@ -1102,6 +1103,13 @@ def swaa_attn_key_weights(q, k, lse, window: int, n_sink: int, n_prompt: int | N
     swaa_attn_key_weights_workspace_bytes(...) bytes (allocated here with torch when None).  Returns weights.
     """
     tc = torch or _torch()
+    if weights is not None and workspace is None and stream is None:
+        r = _host.key_weights(q, k, lse, window, n_sink, n_prompt, scale, weights, decay, cu_seqlens_q, cu_seqlens_k, max_seqlen_q,
+                              max_seqlen_k, seq_lens, block_table, n_prompts)
+        if r is True:
+            return weights
+        if r is not None:
+            raise SwaaError(r, swaa_status_string(r))
     packed, paged = cu_seqlens_q is not None, block_table is not None
     _elements(tc, q, "q", dims=3 if packed else 4)
     _elements(tc, k, "k", q, dims=3 if packed and not paged else 4)
@@ -1149,6 +1157,10 @@ def swaa_cache_evict(k, v, weights, n_keep: int, n_sink: int, n_recent: int, seq
     new_lens int32 [B], the sequences' new lengths; new_lens=seq_lens updates those in place).
     """
     tc = torch or _torch()
+    if kept is None and new_lens is None and stream is None:
+        r = _host.evict(k, v, weights, n_keep, n_sink, n_recent, seq_lens, block_table, max_seqlen_k)
+        if r is not None:
+            return _results(r)
     paged = block_table is not None
     _elements(tc, k, "k")
     _elements(tc, v, "v", k, k.shape[1])

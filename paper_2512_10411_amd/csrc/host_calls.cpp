@@ -439,28 +439,139 @@ PyObject *norm_rope_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// bind_cache(addresses of the three entry points above, sizes of the binding's two argument blocks), behind bind, which has checked
+decltype(&swaa_attn_key_weights) key_weights_entry;
+decltype(&swaa_attn_key_weights_workspace_bytes) key_weights_workspace_entry;
+decltype(&swaa_cache_evict) evict_entry;
+
+// Weights [B, Hkv, >= Nk] with contiguous rows.
+bool plain_weights(PyObject *o, int device, int64_t B, int64_t Hkv, int64_t Nk, float *&data, long long &stride_b, long long &stride_h) {
+    const at::Tensor *t = plain_tensor(o, device);
+    if (!t || t->scalar_type() != at::kFloat || t->dim() != 3 || t->size(0) != B || t->size(1) != Hkv || t->size(2) < Nk || (t->size(2) > 1 && t->stride(2) != 1))
+        return false;
+    data = static_cast<float *>(t->data_ptr());
+    stride_b = B > 1 ? t->stride(0) : 0, stride_h = Hkv > 1 ? t->stride(1) : 0;
+    return true;
+}
+// A block table of B sequences and the pages of `cache`, if there is one.
+template <typename Args>
+bool plain_pages(PyObject *o, int device, int64_t B, const at::Tensor &cache, Args &s) {
+    if (o == Py_None) return true;
+    const at::Tensor *t = plain_tensor(o, device);
+    if (!t || t->scalar_type() != at::kInt || t->dim() != 2 || t->size(0) != B || B < 1 || (t->size(1) > 1 && t->stride(1) != 1)) return false;
+    s.block_table = static_cast<const int *>(t->data_ptr());
+    s.block_table_stride = (int)(B > 1 ? t->stride(0) : t->size(1)), s.page_size = (int)cache.size(2), s.num_pages = (int)cache.size(0);
+    return true;
+}
+
+// key_weights(q, k, lse, window, n_sink, n_prompt, scale, weights, decay, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k, seq_lens,
+// block_table, n_prompts): True
+PyObject *key_weights(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int device;
+    swaa_key_weights_args s{};
+    if (n != 16 || !plain_call(a[0], device, s.stream)) Py_RETURN_NONE;
+    const bool packed = a[9] != Py_None, paged = a[14] != Py_None;
+    const int64_t dims = packed ? 3 : 4;
+    const at::Tensor *q = plain_tensor(a[0], device), *k = plain_tensor(a[1], device);
+    if (!q || (q->scalar_type() != at::kBFloat16 && q->scalar_type() != at::kHalf) || q->dim() != dims || q->stride(-1) != 1) Py_RETURN_NONE;
+    if (!k || k->scalar_type() != q->scalar_type() || k->dim() != (paged ? 4 : dims) || k->stride(-1) != 1 || k->size(-1) != q->size(-1)) Py_RETURN_NONE;
+    const int64_t D = q->size(-1), T = q->size(-2), Hq = q->size(-3), Hkv = k->size(-3), rows = k->size(-2);
+    int64_t B = packed ? 0 : q->size(0);
+    if (!packed && !paged && k->size(0) != B) Py_RETURN_NONE;
+    if (packed) {
+        const at::Tensor *cu_q, *cu_k;
+        if (!plain_vector(a[9], device, -1, cu_q) || !plain_vector(a[10], device, cu_q->numel(), cu_k) || a[13] != Py_None) Py_RETURN_NONE;
+        B = cu_q->numel() - 1;
+        s.cu_seqlens_q = static_cast<const int *>(cu_q->data_ptr()), s.cu_seqlens_k = static_cast<const int *>(cu_k->data_ptr());
+        if (!plain_int(a[11], s.Nq) || !plain_int(a[12], s.Nk)) Py_RETURN_NONE;
+    } else {
+        if (a[10] != Py_None || (paged && a[12] == Py_None)) Py_RETURN_NONE;
+        s.Nq = (int)T, s.Nk = (int)rows;
+        if (a[12] != Py_None && (!plain_int(a[12], s.Nk) || (!paged && s.Nk > rows))) Py_RETURN_NONE;
+        if (!plain_numbers(a[13], device, at::kInt, {B}, s.seq_lens)) Py_RETURN_NONE;
+    }
+    s.B = (int)B, s.Hq = (int)Hq, s.Hkv = (int)Hkv, s.D = (int)D;
+    if (a[2] == Py_None || !(packed ? plain_numbers(a[2], device, at::kFloat, {Hq, T}, s.lse) : plain_numbers(a[2], device, at::kFloat, {B, Hq, T}, s.lse))) Py_RETURN_NONE;
+    s.lse_stride_b = packed ? 0 : Hq * T, s.lse_stride_h = T;
+    s.n_prompt = 0x7fffffff;
+    if (!plain_int(a[3], s.window) || !plain_int(a[4], s.n_sink) || (a[5] != Py_None && !plain_int(a[5], s.n_prompt))) Py_RETURN_NONE;
+    if (!plain_scale(a[6], D, s.scale) || !PyFloat_CheckExact(a[8]) || !plain_pages(a[14], device, B, *k, s)) Py_RETURN_NONE;
+    s.decay = (float)PyFloat_AS_DOUBLE(a[8]);
+    if (!plain_numbers(a[15], device, at::kInt, {B}, s.n_prompts)) Py_RETURN_NONE;
+    if (!plain_weights(a[7], device, B, Hkv, s.Nk, s.weights, s.weights_stride_b, s.weights_stride_h)) Py_RETURN_NONE;
+    s.dtype = q->scalar_type() == at::kHalf ? SWAA_F16 : SWAA_BF16;
+    s.q = rows_of(*q), s.k = rows_of(*k);
+    const long long need = key_weights_workspace_entry(&s);
+    if (need < 0) return PyLong_FromLongLong(need);
+    at::Tensor workspace;
+    if (need > 0) workspace = empty_bytes(*q, need), s.workspace = workspace.data_ptr(), s.workspace_bytes = need;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = key_weights_entry(&s);
+    Py_END_ALLOW_THREADS
+    if (rc != SWAA_OK) return PyLong_FromLong(rc);
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// evict(k, v, weights, n_keep, n_sink, n_recent, seq_lens, block_table, max_seqlen_k): (kept, new_lens)
+PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int device;
+    swaa_evict_args s{};
+    if (n != 9 || !plain_call(a[0], device, s.stream)) Py_RETURN_NONE;
+    const bool paged = a[7] != Py_None;
+    const at::Tensor *k = plain_tensor(a[0], device), *v = plain_tensor(a[1], device);
+    for (const at::Tensor *t : {k, v})
+        if (!t || (t->scalar_type() != at::kBFloat16 && t->scalar_type() != at::kHalf) || t->dim() != 4 || t->stride(3) != 1) Py_RETURN_NONE;
+    if (k->scalar_type() != v->scalar_type() || k->sizes() != v->sizes() || (paged && a[8] == Py_None)) Py_RETURN_NONE;
+    const at::Tensor *table = paged ? plain_tensor(a[7], device) : nullptr;
+    if (paged && (!table || table->dim() != 2)) Py_RETURN_NONE;
+    const int64_t B = paged ? table->size(0) : k->size(0), Hkv = k->size(1);
+    s.B = (int)B, s.Hkv = (int)Hkv, s.D = (int)k->size(3), s.Nk = (int)k->size(2);
+    if (a[8] != Py_None && (!plain_int(a[8], s.Nk) || (!paged && s.Nk > k->size(2)))) Py_RETURN_NONE;
+    if (!plain_int(a[3], s.n_keep) || !plain_int(a[4], s.n_sink) || !plain_int(a[5], s.n_recent) || s.n_keep < 1 || B < 1) Py_RETURN_NONE;
+    if (!plain_numbers(a[6], device, at::kInt, {B}, s.seq_lens) || !plain_pages(a[7], device, B, *k, s)) Py_RETURN_NONE;
+    if (!plain_weights(a[2], device, B, Hkv, s.Nk, s.weights, s.weights_stride_b, s.weights_stride_h)) Py_RETURN_NONE;
+    const at::Tensor kept = at::empty({B, Hkv, s.n_keep}, k->options().dtype(at::kInt)), lens = at::empty({B}, k->options().dtype(at::kInt));
+    s.kept = static_cast<int *>(kept.data_ptr()), s.new_lens = static_cast<int *>(lens.data_ptr());
+    s.k = rows_of(*k), s.v = rows_of(*v);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = evict_entry(&s);
+    Py_END_ALLOW_THREADS
+    return results(rc, kept, lens);
+    END_HANDLE_TH_ERRORS
+}
+
+// bind_cache(addresses of the six entry points above, sizes of the binding's four argument blocks), behind bind, which has checked
 // the library.
 PyObject *bind_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    if (n != 5) {
-        PyErr_SetString(PyExc_TypeError, "bind_cache takes three addresses and two numbers");
+    constexpr int kEntries = 6, kBlocks = 4;
+    static const size_t blocks[kBlocks] = {sizeof(swaa_norm_rope_args), sizeof(swaa_norm_rope_bwd_args), sizeof(swaa_key_weights_args), sizeof(swaa_evict_args)};
+    if (n != kEntries + kBlocks) {
+        PyErr_SetString(PyExc_TypeError, "bind_cache takes six addresses and four numbers");
         return nullptr;
     }
-    void *at[3];
-    for (int i = 0; i < 3; ++i) {
+    void *at[kEntries];
+    for (int i = 0; i < kEntries; ++i) {
         at[i] = PyLong_AsVoidPtr(a[i]);
         if (PyErr_Occurred()) return nullptr;
     }
-    const long long fwd_bytes = PyLong_AsLongLong(a[3]), bwd_bytes = PyLong_AsLongLong(a[4]);
-    if (PyErr_Occurred()) return nullptr;
-    if (fwd_bytes != (long long)sizeof(swaa_norm_rope_args) || bwd_bytes != (long long)sizeof(swaa_norm_rope_bwd_args)) {
-        PyErr_Format(PyExc_ImportError, "compiled for argument blocks of %zu and %zu bytes, not %lld and %lld", sizeof(swaa_norm_rope_args),
-                     sizeof(swaa_norm_rope_bwd_args), fwd_bytes, bwd_bytes);
-        return nullptr;
+    for (int i = 0; i < kBlocks; ++i) {
+        const long long bytes = PyLong_AsLongLong(a[kEntries + i]);
+        if (PyErr_Occurred()) return nullptr;
+        if (bytes != (long long)blocks[i]) {
+            PyErr_Format(PyExc_ImportError, "compiled for an argument block of %zu bytes, not %lld", blocks[i], bytes);
+            return nullptr;
+        }
     }
     norm_rope_entry = reinterpret_cast<decltype(norm_rope_entry)>(at[0]);
     norm_rope_bwd_entry = reinterpret_cast<decltype(norm_rope_bwd_entry)>(at[1]);
     norm_rope_bwd_workspace_entry = reinterpret_cast<decltype(norm_rope_bwd_workspace_entry)>(at[2]);
+    key_weights_entry = reinterpret_cast<decltype(key_weights_entry)>(at[3]);
+    key_weights_workspace_entry = reinterpret_cast<decltype(key_weights_workspace_entry)>(at[4]);
+    evict_entry = reinterpret_cast<decltype(evict_entry)>(at[5]);
     Py_RETURN_NONE;
 }
 
@@ -503,7 +614,8 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {METHOD(bind), METHOD(bind_cache), METHOD(fwd), METHOD(decode), METHOD(decode_ex), METHOD(fill_fwd_ex), METHOD(norm_rope), METHOD(norm_rope_bwd), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {METHOD(bind), METHOD(bind_cache), METHOD(fwd), METHOD(decode), METHOD(decode_ex), METHOD(fill_fwd_ex), METHOD(norm_rope), METHOD(norm_rope_bwd),
+                         METHOD(key_weights), METHOD(evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -96,13 +96,13 @@ struct KeyWeightsParams {
     float scale_log2, decay;
     // Work (plan_key_weights): (sequence, KV head) pairs x (tiles of keys x chunks of the columns, heads of the group x rows that see
     // the tile).  A row sees few keys of a windowed layer, but the sinks are seen by all: their tiles have chunk counts of their own.
+    int key_tile, one_stage, listed;  // keys of a workgroup; at most one stage of columns; tiles by a list of the sequences' own
     int pairs, tiles, sink_tiles, sink_items;
     int chunks, sink_chunks, chunk_stages;  // (stages of 64 columns)
     long long items;
     FastDiv div_pairs, div_hkv, div_sink_chunks, div_others;
-    float *partial;  // [items][keys of a tile], or null: one chunk per tile
+    float *partial;  // [items][key_tile], or null: one chunk per tile
 };
-constexpr int kKeyTile = 256;  // keys of a workgroup
 bool plan_key_weights(KeyWeightsParams &p);
 long long key_weights_workspace_bytes(const KeyWeightsParams &p);
 hipError_t launch_key_weights(const KeyWeightsParams &p, hipStream_t stream);

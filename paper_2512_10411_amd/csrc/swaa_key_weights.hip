@@ -16,6 +16,8 @@ namespace {
 
 constexpr int kWThreads = 256;
 constexpr int kMinChunk = 256;    // columns a workgroup goes through at least, if there are as many
+constexpr int kFewColumns = 256;  // up to here a wave has 32 keys instead of 64
+constexpr int kListedWgs = 1024;  // workgroups that go through a list of tiles (one per tile of the longest sequence instead: 47.8 -> 39.0 us, 16 of 0.2-16k)
 constexpr int kFillItems = 4096;  // workgroups that a call should have
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -68,6 +70,30 @@ __device__ __forceinline__ Item item_of(const KeyWeightsParams &p, unsigned id) 
     w.kvh = (int)(pair - (unsigned)w.b * (unsigned)(p.pairs / p.seq.B));
     return w;
 }
+// Sequences of different lengths whose tiles are whole (p.listed): item `id` of the list that holds every sequence's own tiles, one
+// sequence behind the other; false behind its end.  Every wave reads the lengths, 64 at a time.
+__device__ __forceinline__ bool listed_item(const KeyWeightsParams &p, unsigned id, int key_tile, Item &w) {
+    const int lane = threadIdx.x & 63, hkv = p.pairs / p.seq.B;
+    const unsigned tile = fastdiv(id, p.div_hkv);
+    unsigned before = 0;
+    for (int c0 = 0; c0 < p.seq.B; c0 += 64) {
+        int nq, nk;
+        sequence(p.seq, min(c0 + lane, p.seq.B - 1), nq, nk);
+        const unsigned incl = wave_inclusive_scan(c0 + lane < p.seq.B ? (unsigned)(nk + key_tile - 1) / (unsigned)key_tile : 0u);
+        const unsigned all = wave_read_lane(incl, 63);
+        if (tile - before < all) {
+            const int n = __popcll(__ballot(incl <= tile - before));  // sequences among these that end at or before the tile
+            w.b = __builtin_amdgcn_readfirstlane(c0 + n);
+            w.tile = __builtin_amdgcn_readfirstlane((int)(tile - before - (n ? wave_read_lane(incl, n - 1) : 0u)));
+            w.kvh = (int)(id - tile * (unsigned)hkv);
+            w.chunk = 0;
+            w.whole = true;
+            return true;
+        }
+        before += all;
+    }
+    return false;
+}
 
 // The columns of a tile, kCols to a stage: head by head, each one's rows from the start of a stage on, or, where a head has few, all
 // heads' in a row.
@@ -82,8 +108,8 @@ struct Columns {
     }
 };
 
-// LDS: two buffers of kCols rows of Q without padding, then two of what the keys are told about each column: its lse in log2 units,
-// `pos` and `lo` (its row sees the keys up to pos that lie above lo, and the sinks; pos -1: nothing, no such column).  16-byte
+// LDS: two buffers of what the keys are told about each column -- its lse in log2 units, `pos` and `lo` (its row sees the keys up to
+// pos that lie above lo, and the sinks; pos -1: nothing, no such column) -- then two of kCols rows of Q without padding.  16-byte
 // chunk c of row r lies at chunk c ^ turn(r), so that the equal chunks of 16 rows lie in different banks (64 of 4 bytes); the copies
 // apply it on the global side.
 __host__ __device__ constexpr int stage_cols(int D) { return D <= 128 ? 64 : 32; }
@@ -91,8 +117,9 @@ template <int D>
 struct Stage {
     static constexpr int kCols = stage_cols(D);
     static constexpr int kRowB = D * 2, kBufB = kCols * kRowB;
-    static constexpr int kLse = 2 * kBufB, kPos = kLse + 2 * kCols * 4, kLo = kPos + 2 * kCols * 4;  // byte addresses
-    static constexpr int kBytes = kLo + 2 * kCols * 4;
+    static constexpr int kLse = 0, kPos = kLse + 2 * kCols * 4, kLo = kPos + 2 * kCols * 4;  // byte addresses
+    static constexpr int kRows = kLo + 2 * kCols * 4;
+    static constexpr int kBytes = kRows + 2 * kBufB, kOneStage = kRows + kBufB;  // (calls of one stage have no use for the second buffer)
     static __device__ __forceinline__ int turn(int r) { return D % 128 == 0 ? r & 15 : D % 64 == 0 ? (r >> 1) & 7 : (r >> 2) & 3; }
 };
 
@@ -103,24 +130,27 @@ __device__ __forceinline__ X lds_word(const LdsByte *at) { return *(const X __at
 template <typename X>
 __device__ __forceinline__ void lds_put(LdsByte *at, X x) { *(X __attribute__((address_space(3))) *)at = x; }
 
-template <int D, bool kF16>
-__global__ __launch_bounds__(kWThreads, D <= 128 ? 3 : 2) void swaa_key_weights_kernel(const KeyWeightsParams p) {
+// One item: kM blocks of 16 keys to a wave.
+template <int D, bool kF16, int kM>
+__device__ __forceinline__ void weigh_item(const KeyWeightsParams &p, const Item &it, unsigned id) {
     using T = Stage<D>;
-    constexpr int kM = 4;                       // 16-key blocks of a wave
     constexpr int kWaveKeys = 16 * kM;
     constexpr int KS = D / 32;                  // k-steps of a product
     constexpr int kCols = T::kCols, kWaveCols = kCols / 4;  // columns that a wave brings
     constexpr int kChunks = D / 8;              // of 16 bytes in a row
     constexpr int kCopies = (kWaveCols * kChunks + 63) / 64;  // wave instructions for them
-    static_assert(kKeyTile == 4 * kWaveKeys, "");
+    constexpr int kTile = 4 * kWaveKeys;
 
-    const Item it = item_of(p, blockIdx.x);
     int nq, nk;
     sequence(p.seq, it.b, nq, nk);
-    const int k0 = it.tile * kKeyTile;
+    // (the same in all lanes; the compiler has to know it for the addresses of the copies)
+    nq = __builtin_amdgcn_readfirstlane(nq);
+    nk = __builtin_amdgcn_readfirstlane(nk);
+    const int k0 = it.tile * kTile;
     if (k0 >= nk) return;
-    const int P = p.n_prompts ? max(p.n_prompts[it.b], 0) : p.P;
-    const SeenBy seen = seen_by(k0, min(k0 + kKeyTile, nk), nq, nk, p.W, p.S, P);
+    const int P = p.n_prompts ? __builtin_amdgcn_readfirstlane(max(p.n_prompts[it.b], 0)) : p.P;
+    const int q_row0 = p.seq.cu_q ? __builtin_amdgcn_readfirstlane(p.seq.cu_q[it.b]) : 0;  // of packed sequences
+    const SeenBy seen = seen_by(k0, min(k0 + kTile, nk), nq, nk, p.W, p.S, P);
     const Columns<kCols> cols(seen.n_all, p.G);
     const int s_begin = it.chunk * p.chunk_stages * (64 / kCols), s_end = min(cols.stages, s_begin + p.chunk_stages * (64 / kCols));
     if (it.chunk > 0 && s_begin >= s_end) return;
@@ -153,8 +183,8 @@ __global__ __launch_bounds__(kWThreads, D <= 128 ? 3 : 2) void swaa_key_weights_
 
     // ---- columns, a stage at a time; a wave brings kWaveCols of them
     const char *q_base = p.q.ptr + 2 * ((packed ? 0 : it.b * p.q.sb) + it.kvh * (long long)p.G * p.q.sh +
-                                        (packed ? p.seq.cu_q[it.b] * p.q.sn : 0));
-    const float *lse_base = p.lse + (packed ? p.seq.cu_q[it.b] : it.b * p.lse_sb) + it.kvh * (long long)p.G * p.lse_sh;
+                                        q_row0 * p.q.sn);
+    const float *lse_base = p.lse + (packed ? q_row0 : it.b * p.lse_sb) + it.kvh * (long long)p.G * p.lse_sh;
     const int off = nk - nq;
     // (of instruction i: row 64 i + lane of kChunks chunks each of the wave's columns, chunk of LDS, and its address behind row 0's)
     uint32_t copy_at[kCopies];
@@ -178,7 +208,7 @@ __global__ __launch_bounds__(kWThreads, D <= 128 ? 3 : 2) void swaa_key_weights_
         valid = min(kCols, (cols.by_head ? seen.n_all : seen.n_all * p.G) - index);
         straight = cols.by_head && valid == kCols && (index + kCols <= seen.n || index >= seen.n);
         row0 = seen.row(index);
-        const uint32_t to = (uint32_t)(buf * T::kBufB + wave * kWaveCols * T::kRowB);
+        const uint32_t to = (uint32_t)(T::kRows + buf * T::kBufB + wave * kWaveCols * T::kRowB);
         const int mine = wave * kWaveCols + lane % kWaveCols;
         if (straight) {
             const char *src = q_base + 2 * (head * p.q.sh + row0 * p.q.sn);
@@ -264,7 +294,7 @@ __global__ __launch_bounds__(kWThreads, D <= 128 ? 3 : 2) void swaa_key_weights_
         }
         LdsByte *at[KS], *const col_at = lds_at((uint32_t)(T::kLse + 4 * (buf * kCols + l16)));
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) at[ks] = lds_at(q_at[ks] + (uint32_t)(buf * T::kBufB));
+        for (int ks = 0; ks < KS; ++ks) at[ks] = lds_at(q_at[ks] + (uint32_t)(T::kRows + buf * T::kBufB));
         if (all) {
 #pragma unroll
             for (int t = 0; t < kCols / 16; ++t) {
@@ -318,53 +348,75 @@ __global__ __launch_bounds__(kWThreads, D <= 128 ? 3 : 2) void swaa_key_weights_
         for (int e = 0; e < 4; ++e)
             if (l16 == 4 * m + e) mine = sum[m][e];
     const int of_tile = wave * kWaveKeys + 16 * (l16 >> 2) + 4 * quad + (l16 & 3);
+    if (l16 >= 4 * kM) return;
     if (!it.whole) {
-        p.partial[(long long)blockIdx.x * kKeyTile + of_tile] = mine;
+        p.partial[(long long)id * kTile + of_tile] = mine;
     } else if (k0 + of_tile < nk) {
         float *w = p.weights + it.b * p.w_sb + it.kvh * p.w_sh + k0 + of_tile;
         *w = p.decay != 0.f ? p.decay * *w + mine : mine;
     }
 }
 
+// Waves of a SIMD: what the registers allow.
+constexpr int weigh_waves(int D, int kM) { return D > 128 ? 2 : kM == 2 ? 5 : 3; }
+template <int D, bool kF16, int kM>
+__global__ __launch_bounds__(kWThreads, weigh_waves(D, kM)) void swaa_key_weights_kernel(const KeyWeightsParams p) {
+    fetch_args<KeyWeightsParams>();
+    weigh_item<D, kF16, kM>(p, item_of(p, blockIdx.x), blockIdx.x);
+}
+template <int D, bool kF16, int kM>
+__global__ __launch_bounds__(kWThreads, kM == 2 && D <= 128 ? 4 : weigh_waves(D, kM)) void swaa_key_weights_listed_kernel(const KeyWeightsParams p) {
+    fetch_args<KeyWeightsParams>();
+    Item it;
+    for (unsigned id = blockIdx.x; listed_item(p, id, 64 * kM, it); id += gridDim.x) {
+        weigh_item<D, kF16, kM>(p, it, id);
+        __syncthreads();  // (the next item's columns go where this one's were)
+    }
+}
+
 // Chunks of a tile's columns added up in their order (tiles of several chunks: those of the sinks, or all).
-__global__ __launch_bounds__(kKeyTile) void swaa_key_weights_merge_kernel(const KeyWeightsParams p) {
+__global__ __launch_bounds__(256) void swaa_key_weights_merge_kernel(const KeyWeightsParams p) {
     const unsigned tile = fastdiv(blockIdx.x, p.div_pairs), pair = blockIdx.x - tile * (unsigned)p.pairs;
     const int b = (int)fastdiv(pair, p.div_hkv), kvh = (int)(pair - (unsigned)b * (unsigned)(p.pairs / p.seq.B));
     int nq, nk;
     sequence(p.seq, b, nq, nk);
-    const int k0 = (int)tile * kKeyTile, key = k0 + (int)threadIdx.x;
+    const int k0 = (int)tile * p.key_tile, key = k0 + (int)threadIdx.x;
     if (key >= nk) return;
     const int P = p.n_prompts ? max(p.n_prompts[b], 0) : p.P;
-    const SeenBy seen = seen_by(k0, min(k0 + kKeyTile, nk), nq, nk, p.W, p.S, P);
+    const SeenBy seen = seen_by(k0, min(k0 + p.key_tile, nk), nq, nk, p.W, p.S, P);
     const bool narrow = stage_cols(p.D) == 32;
     const int stages = narrow ? Columns<32>(seen.n_all, p.G).stages : Columns<64>(seen.n_all, p.G).stages;
     const int of_chunk = p.chunk_stages * (narrow ? 2 : 1);
     const bool has_sinks = (int)tile < p.sink_tiles;
     // its first chunk's place among the pair's items, and from chunk to chunk
     const long long first = has_sinks ? (long long)tile * p.sink_chunks : p.sink_items + ((long long)tile - p.sink_tiles);
-    const long long step = (has_sinks ? 1LL : p.tiles - p.sink_tiles) * p.pairs * kKeyTile;
+    const long long step = (has_sinks ? 1LL : p.tiles - p.sink_tiles) * p.pairs * p.key_tile;
     const int chunks = has_sinks ? p.sink_chunks : p.chunks;
-    const float *src = p.partial + (first * p.pairs + pair) * kKeyTile + threadIdx.x;
+    const float *src = p.partial + (first * p.pairs + pair) * p.key_tile + threadIdx.x;
     float x = src[0];
     for (int c = 1; c < chunks && c * of_chunk < stages; ++c) x += src[c * step];
     float *w = p.weights + b * p.w_sb + kvh * p.w_sh + key;
     *w = p.decay != 0.f ? p.decay * *w + x : x;
 }
 
-template <int D, bool kF16>
+template <int D, bool kF16, int kM>
 hipError_t launch_one(const KeyWeightsParams &p, hipStream_t stream) {
-    constexpr auto kernel = swaa_key_weights_kernel<D, kF16>;
     static_assert(Stage<D>::kBytes <= 64 * 1024, "");
-    kernel<<<dim3((unsigned)p.items), dim3(kWThreads), Stage<D>::kBytes, stream>>>(p);
+    const int lds = p.one_stage ? Stage<D>::kOneStage : Stage<D>::kBytes;
+    if (p.listed)
+        swaa_key_weights_listed_kernel<D, kF16, kM><<<dim3((unsigned)(p.items < kListedWgs ? p.items : kListedWgs)), dim3(kWThreads), lds, stream>>>(p);
+    else
+        swaa_key_weights_kernel<D, kF16, kM><<<dim3((unsigned)p.items), dim3(kWThreads), lds, stream>>>(p);
     return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch(const KeyWeightsParams &p, hipStream_t stream) {
-    const hipError_t err = p.fp16 ? launch_one<D, true>(p, stream) : launch_one<D, false>(p, stream);
+    const hipError_t err = p.key_tile == 128 ? (p.fp16 ? launch_one<D, true, 2>(p, stream) : launch_one<D, false, 2>(p, stream))
+                                             : (p.fp16 ? launch_one<D, true, 4>(p, stream) : launch_one<D, false, 4>(p, stream));
     const int merged = p.chunks > 1 ? p.tiles : p.sink_chunks > 1 ? p.sink_tiles : 0;
     if (err != hipSuccess || merged == 0) return err;
-    swaa_key_weights_merge_kernel<<<dim3((unsigned)((long long)p.pairs * merged)), dim3(kKeyTile), 0, stream>>>(p);
+    swaa_key_weights_merge_kernel<<<dim3((unsigned)((long long)p.pairs * merged)), dim3((unsigned)p.key_tile), 0, stream>>>(p);
     return hipGetLastError();
 }
 
@@ -373,18 +425,20 @@ hipError_t launch(const KeyWeightsParams &p, hipStream_t stream) {
 // The columns of all tiles, shared out in chunks of one length so that the call has as many workgroups as the chip wants.
 bool plan_key_weights(KeyWeightsParams &p) {
     const int Nq = p.seq.Nq, Nk = p.seq.Nk;
-    p.pairs = p.seq.B * (p.Hq / p.G);
-    p.tiles = (Nk + kKeyTile - 1) / kKeyTile;
     if ((long long)p.G * (Nq + 64LL) > 0x3fffffffLL) return false;
+    p.key_tile = (long long)p.G * Nq <= kFewColumns ? 128 : 256;
+    p.one_stage = (long long)p.G * Nq <= stage_cols(p.D);
+    p.pairs = p.seq.B * (p.Hq / p.G);
+    p.tiles = (Nk + p.key_tile - 1) / p.key_tile;
     // stages (of 64 columns) of a tile seen by n rows, at most
     auto stages_of = [&](long long n) { return Columns<64>((int)(n < Nq ? n : Nq), p.G).stages; };
     const int most = stages_of(Nq);
     // rows that see a tile without sinks: those of its window, and generated ones (of sequences with prompt lengths of their own: maybe all)
     const long long generated = p.n_prompts ? Nk : Nk - p.P;
-    const long long of_window = (long long)p.W + kKeyTile - 1 + generated;
+    const long long of_window = (long long)p.W + p.key_tile - 1 + generated;
     const int usual = stages_of(of_window);
-    p.sink_tiles = usual < most ? (p.S + kKeyTile - 1) / kKeyTile : 0;
-    const bool ramp = of_window >= Nq && Nq > kKeyTile;  // (a whole prompt's rows: the last tiles see few)
+    p.sink_tiles = usual < most ? (p.S + p.key_tile - 1) / p.key_tile : 0;
+    const bool ramp = of_window >= Nq && Nq > p.key_tile;  // (a whole prompt's rows: the last tiles see few)
     const long long all = p.pairs * ((long long)(p.tiles - p.sink_tiles) * (ramp ? usual / 2 + 1 : usual) + (long long)p.sink_tiles * most);
     const long long chunk = (all + kFillItems - 1) / kFillItems;
     p.chunk_stages = (int)(chunk > kMinChunk / 64 ? chunk : kMinChunk / 64);
@@ -392,7 +446,8 @@ bool plan_key_weights(KeyWeightsParams &p) {
     p.sink_chunks = (most + p.chunk_stages - 1) / p.chunk_stages;
     p.sink_items = p.sink_tiles * p.sink_chunks;
     p.items = (long long)p.pairs * (p.sink_items + (long long)(p.tiles - p.sink_tiles) * p.chunks);
-    if (p.items > 0x7fffffffLL) return false;
+    p.listed = p.chunks == 1 && p.sink_chunks == 1 && (p.seq.seq_lens || p.seq.cu_k);
+    if (p.items > 0x7fffffffLL - kListedWgs) return false;
     p.div_pairs = make_fastdiv((unsigned)p.pairs);
     p.div_hkv = make_fastdiv((unsigned)(p.Hq / p.G));
     p.div_sink_chunks = make_fastdiv((unsigned)p.sink_chunks);
@@ -404,7 +459,7 @@ bool plan_key_weights(KeyWeightsParams &p) {
 // tiles of sinks, and rounding adds at most one chunk to each.  16 MiB are never reached.)
 long long key_weights_workspace_bytes(const KeyWeightsParams &p) {
     const long long items = p.chunks > 1 ? p.items : p.sink_chunks > 1 ? (long long)p.pairs * p.sink_items : 0;
-    return items * kKeyTile * (long long)sizeof(float);
+    return items * p.key_tile * (long long)sizeof(float);
 }
 
 hipError_t launch_key_weights(const KeyWeightsParams &p, hipStream_t stream) {
