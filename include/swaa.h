@@ -545,6 +545,8 @@ long long swaa_attn_key_weights_workspace_bytes(const swaa_key_weights_args *arg
  *   kept       device ints [B, Hkv, n_keep], contiguous, written: the rows that stayed, ascending; -1 behind a shorter sequence's
  *   new_lens   device, B ints, written: min(len, n_keep), the new number of cached tokens; may be seq_lens itself, or NULL
  *   n_keep >= 1; n_sink, n_recent >= 0 with n_sink + n_recent <= n_keep
+ *   workspace  device scratch memory owned by the caller, 16-byte aligned, at least swaa_cache_evict_workspace_bytes(args) bytes, or
+ *              NULL: the same results, slower for long sequences; calls that may overlap on the device need separate workspaces
  *
  * The rows of a sequence no longer stand at their positions: attention over it takes window >= Nk, and new tokens pass their
  * positions to swaa_qk_norm_rope.  Returns SWAA_OK or a negative swaa_status.
@@ -559,10 +561,15 @@ typedef struct swaa_evict_args {
     int n_keep, n_sink, n_recent;
     const int *block_table;
     int block_table_stride, page_size, num_pages;
+    void *workspace;
+    long long workspace_bytes;
     void *stream;
 } swaa_evict_args;
 
 int swaa_cache_evict(const swaa_evict_args *args);
+
+/* Bytes of workspace swaa_cache_evict has use for (0 for short sequences, or many): reads B, Hkv, D and Nk.  Host-only arithmetic. */
+long long swaa_cache_evict_workspace_bytes(const swaa_evict_args *args);
 
 /* Static description of a status code; never NULL, never freed. */
 const char *swaa_status_string(int status);

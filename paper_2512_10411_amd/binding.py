@@ -34,7 +34,7 @@ EXPORTS = ("swaa_attn_fwd", "swaa_attn_fwd_fa_decode", "swaa_attn_fwd_ex", "swaa
            "swaa_visible_pairs_fa_decode",
            "swaa_attn_decode", "swaa_attn_decode_ex", "swaa_attn_decode_workspace_bytes", "swaa_attn_decode_ex_workspace_bytes", "swaa_attn_decode_static", "swaa_attn_bwd", "swaa_attn_bwd_workspace_bytes",
            "swaa_qk_norm_rope", "swaa_qk_norm_rope_bwd", "swaa_qk_norm_rope_bwd_workspace_bytes",
-           "swaa_attn_key_weights", "swaa_attn_key_weights_workspace_bytes", "swaa_cache_evict",
+           "swaa_attn_key_weights", "swaa_attn_key_weights_workspace_bytes", "swaa_cache_evict", "swaa_cache_evict_workspace_bytes",
            "swaa_status_string", "swaa_version")
 
 _lib = None
@@ -120,7 +120,8 @@ class SwaaEvictArgs(ctypes.Structure):
                 ("B", ctypes.c_int), ("Hkv", ctypes.c_int), ("D", ctypes.c_int), ("Nk", ctypes.c_int),
                 ("n_keep", ctypes.c_int), ("n_sink", ctypes.c_int), ("n_recent", ctypes.c_int),
                 ("block_table", ctypes.c_void_p), ("block_table_stride", ctypes.c_int), ("page_size", ctypes.c_int),
-                ("num_pages", ctypes.c_int), ("stream", ctypes.c_void_p)]
+                ("num_pages", ctypes.c_int),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_longlong), ("stream", ctypes.c_void_p)]
 
 
 class SwaaError(RuntimeError):
@@ -180,7 +181,8 @@ def load_library() -> ctypes.CDLL:
                         ("attn_key_weights", SwaaKeyWeightsArgs), ("cache_evict", SwaaEvictArgs)):
         call = getattr(lib, "swaa_" + name)
         call.restype, call.argtypes = ctypes.c_int, [ctypes.POINTER(block)]
-    for name, block in (("qk_norm_rope_bwd", SwaaNormRopeBwdArgs), ("attn_key_weights", SwaaKeyWeightsArgs)):
+    for name, block in (("qk_norm_rope_bwd", SwaaNormRopeBwdArgs), ("attn_key_weights", SwaaKeyWeightsArgs),
+                        ("cache_evict", SwaaEvictArgs)):
         call = getattr(lib, f"swaa_{name}_workspace_bytes")
         call.restype, call.argtypes = ctypes.c_longlong, [ctypes.POINTER(block)]
     lib.swaa_status_string.restype = ctypes.c_char_p
@@ -246,7 +248,7 @@ def _native_part(torch):
             lib.swaa_version(), ctypes.sizeof(SwaaFwdArgs), ctypes.sizeof(SwaaDecodeArgs), str(torch.__version__))
         _host_calls.bind_cache(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
             lib.swaa_qk_norm_rope, lib.swaa_qk_norm_rope_bwd, lib.swaa_qk_norm_rope_bwd_workspace_bytes,
-            lib.swaa_attn_key_weights, lib.swaa_attn_key_weights_workspace_bytes, lib.swaa_cache_evict)),
+            lib.swaa_attn_key_weights, lib.swaa_attn_key_weights_workspace_bytes, lib.swaa_cache_evict, lib.swaa_cache_evict_workspace_bytes)),
             *(ctypes.sizeof(block) for block in (SwaaNormRopeArgs, SwaaNormRopeBwdArgs, SwaaKeyWeightsArgs, SwaaEvictArgs)))
     except (ImportError, TypeError, AttributeError) as e:  # (TypeError: its `bind` takes other arguments; AttributeError: it lacks one)
         warnings.warn(f"{HOST_CALLS_PATH} is not used, calls take longer on the way to the library ({e}): "
@@ -1080,6 +1082,16 @@ def swaa_attn_key_weights_workspace_bytes(B, Hq, Hkv, Nq, Nk, D, window, n_sink,
     return r
 
 
+def swaa_cache_evict_workspace_bytes(B, Hkv, Nk, D) -> int:
+    """Bytes of device scratch swaa_cache_evict has use for with this cache (0 for short sequences, or many)."""
+    a = SwaaEvictArgs()
+    a.B, a.Hkv, a.Nk, a.D = int(B), int(Hkv), int(Nk), int(D)
+    r = int(load_library().swaa_cache_evict_workspace_bytes(ctypes.byref(a)))
+    if r < 0:
+        raise SwaaError(r, swaa_status_string(r))
+    return r
+
+
 def _fill_weights(tc, a, weights, B, Hkv, Nk, like):
     if weights.dtype is not tc.float32 or weights.dim() != 3 or weights.get_device() != like.get_device() \
             or weights.shape[0] != B or weights.shape[1] != Hkv or weights.shape[2] < Nk \
@@ -1147,17 +1159,18 @@ def swaa_attn_key_weights(q, k, lse, window: int, n_sink: int, n_prompt: int | N
 
 
 def swaa_cache_evict(k, v, weights, n_keep: int, n_sink: int, n_recent: int, seq_lens=None, block_table=None,
-                     max_seqlen_k: int | None = None, kept=None, new_lens=None, stream=None):
+                     max_seqlen_k: int | None = None, kept=None, new_lens=None, workspace=None, stream=None):
     """Cuts every sequence of a cache that is longer than n_keep tokens to n_keep rows, per KV head: the first n_sink, the last
     n_recent and the heaviest others by `weights` (swaa_attn_key_weights); they close up in place, weights with them.
 
     k, v: bf16 or fp16 cache views [B, Hkv, Nk, D], or pages [num_pages, Hkv, page_size, D] with block_table (pages that no two
     sequences share) and max_seqlen_k; weights fp32 [B, Hkv, >= Nk] with contiguous rows; seq_lens int32 [B] or None (Nk each).
-    All three are changed in place.  Returns (kept int32 [B, Hkv, n_keep], the rows that stayed, -1 behind shorter sequences',
+    All three are changed in place.  workspace: a uint8 tensor of swaa_cache_evict_workspace_bytes(...) bytes (allocated here with torch
+    when None and the call has use for one).  Returns (kept int32 [B, Hkv, n_keep], the rows that stayed, -1 behind shorter sequences',
     new_lens int32 [B], the sequences' new lengths; new_lens=seq_lens updates those in place).
     """
     tc = torch or _torch()
-    if kept is None and new_lens is None and stream is None:
+    if kept is None and new_lens is None and workspace is None and stream is None:
         r = _host.evict(k, v, weights, n_keep, n_sink, n_recent, seq_lens, block_table, max_seqlen_k)
         if r is not None:
             return _results(r)
@@ -1190,6 +1203,7 @@ def swaa_cache_evict(k, v, weights, n_keep: int, n_sink: int, n_recent: int, seq
             made.append(new_lens)
         a.kept = _numbers(tc, kept, "kept", tc.int32, (a.B, a.Hkv, max(a.n_keep, 0)), k)
         a.new_lens = _numbers(tc, new_lens, "new_lens", tc.int32, (a.B,), k)
+        workspace = _scratch(tc, "swaa_cache_evict", a, workspace, k.device)
         a.stream = _stream_handle(stream, k)
         _call("swaa_cache_evict", a)
         if stream is not None and made:

@@ -442,6 +442,7 @@ PyObject *norm_rope_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
 decltype(&swaa_attn_key_weights) key_weights_entry;
 decltype(&swaa_attn_key_weights_workspace_bytes) key_weights_workspace_entry;
 decltype(&swaa_cache_evict) evict_entry;
+decltype(&swaa_cache_evict_workspace_bytes) evict_workspace_entry;
 
 // Weights [B, Hkv, >= Nk] with contiguous rows.
 bool plain_weights(PyObject *o, int device, int64_t B, int64_t Hkv, int64_t Nk, float *&data, long long &stride_b, long long &stride_h) {
@@ -536,6 +537,10 @@ PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const at::Tensor kept = at::empty({B, Hkv, s.n_keep}, k->options().dtype(at::kInt)), lens = at::empty({B}, k->options().dtype(at::kInt));
     s.kept = static_cast<int *>(kept.data_ptr()), s.new_lens = static_cast<int *>(lens.data_ptr());
     s.k = rows_of(*k), s.v = rows_of(*v);
+    const long long need = evict_workspace_entry(&s);
+    if (need < 0) return PyLong_FromLongLong(need);
+    at::Tensor workspace;
+    if (need > 0) workspace = empty_bytes(*k, need), s.workspace = workspace.data_ptr(), s.workspace_bytes = need;
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = evict_entry(&s);
@@ -544,13 +549,13 @@ PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// bind_cache(addresses of the six entry points above, sizes of the binding's four argument blocks), behind bind, which has checked
+// bind_cache(addresses of the seven entry points above, sizes of the binding's four argument blocks), behind bind, which has checked
 // the library.
 PyObject *bind_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    constexpr int kEntries = 6, kBlocks = 4;
+    constexpr int kEntries = 7, kBlocks = 4;
     static const size_t blocks[kBlocks] = {sizeof(swaa_norm_rope_args), sizeof(swaa_norm_rope_bwd_args), sizeof(swaa_key_weights_args), sizeof(swaa_evict_args)};
     if (n != kEntries + kBlocks) {
-        PyErr_SetString(PyExc_TypeError, "bind_cache takes six addresses and four numbers");
+        PyErr_SetString(PyExc_TypeError, "bind_cache takes seven addresses and four numbers");
         return nullptr;
     }
     void *at[kEntries];
@@ -572,6 +577,7 @@ PyObject *bind_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
     key_weights_entry = reinterpret_cast<decltype(key_weights_entry)>(at[3]);
     key_weights_workspace_entry = reinterpret_cast<decltype(key_weights_workspace_entry)>(at[4]);
     evict_entry = reinterpret_cast<decltype(evict_entry)>(at[5]);
+    evict_workspace_entry = reinterpret_cast<decltype(evict_workspace_entry)>(at[6]);
     Py_RETURN_NONE;
 }
 

@@ -636,12 +636,37 @@ int swaa_attn_key_weights(const swaa_key_weights_args *a) {
     return swaa::launch_key_weights(p, static_cast<hipStream_t>(a->stream)) == hipSuccess ? SWAA_OK : SWAA_ERR_LAUNCH;
 }
 
+namespace {
+
+int evict_plan(const swaa_evict_args *a, swaa::EvictParams &p, long long &ws_bytes) {
+    const int rc = check_heads(a->B, a->Hkv, a->Hkv, a->D);
+    if (rc != SWAA_OK) return rc;
+    if (a->Nk < 1 || a->Nk > (1 << 28)) return SWAA_ERR_SHAPE;  // (weights of a head below 2 GiB)
+    if ((long long)a->B * a->Hkv > 0x7fffffffLL / 256) return SWAA_ERR_SHAPE;
+    p.B = a->B;
+    p.Hkv = a->Hkv;
+    p.D = a->D;
+    p.Nk = a->Nk;
+    ws_bytes = swaa::plan_evict(p);
+    return SWAA_OK;
+}
+
+}  // namespace
+
+long long swaa_cache_evict_workspace_bytes(const swaa_evict_args *a) {
+    if (!a) return SWAA_ERR_NULL;
+    swaa::EvictParams p{};
+    long long bytes = 0;
+    const int rc = evict_plan(a, p, bytes);
+    return rc != SWAA_OK ? rc : bytes;
+}
+
 int swaa_cache_evict(const swaa_evict_args *a) {
     if (!a) return SWAA_ERR_NULL;
     if (!a->k.ptr || !a->v.ptr || !a->weights || !a->kept) return SWAA_ERR_NULL;
-    int rc = check_heads(a->B, a->Hkv, a->Hkv, a->D);
     swaa::EvictParams p{};
-    if (rc == SWAA_OK && a->Nk < 1) rc = SWAA_ERR_SHAPE;
+    long long need = 0;
+    int rc = evict_plan(a, p, need);
     if (rc == SWAA_OK) rc = set_pages(p.pages, a->block_table, a->block_table_stride, a->page_size, a->num_pages, a->Nk);
     if (rc != SWAA_OK) return rc;
     if (a->n_keep < 1 || a->n_sink < 0 || a->n_recent < 0 || (long long)a->n_sink + a->n_recent > a->n_keep) return SWAA_ERR_SHAPE;
@@ -650,8 +675,9 @@ int swaa_cache_evict(const swaa_evict_args *a) {
     for (const void *ptr : {(const void *)a->weights, (const void *)a->kept, (const void *)a->new_lens, (const void *)a->seq_lens})
         if (misaligned_words(ptr)) return SWAA_ERR_ALIGN;
     if ((a->Hkv > 1 && a->weights_stride_h < a->Nk) || (a->B > 1 && a->weights_stride_b < a->Nk)) return SWAA_ERR_SHAPE;
-    if ((long long)a->B * a->Hkv > 0x7fffffffLL / 256 || a->Nk > (1 << 28) || a->B * (long long)a->Hkv * (a->n_keep / 32 + 1LL) > 0x3fffffffLL)
-        return SWAA_ERR_SHAPE;  // (one launch; weights of a head below 2 GiB)
+    if (a->B * (long long)a->Hkv * (a->n_keep / 32 + 1LL) > 0x3fffffffLL) return SWAA_ERR_SHAPE;
+    if (a->workspace && (misaligned(a->workspace) || a->workspace_bytes < need)) return SWAA_ERR_WORKSPACE;
+    p.select_space = need > 0 ? static_cast<unsigned *>(a->workspace) : nullptr;
     p.k = rows_of(a->k);
     p.v = rows_of(a->v);
     p.weights = a->weights;
@@ -660,10 +686,6 @@ int swaa_cache_evict(const swaa_evict_args *a) {
     p.kept = a->kept;
     p.new_lens = a->new_lens;
     p.seq_lens = a->seq_lens;
-    p.B = a->B;
-    p.Hkv = a->Hkv;
-    p.D = a->D;
-    p.Nk = a->Nk;
     p.n_keep = a->n_keep;
     p.n_sink = a->n_sink;
     p.n_recent = a->n_recent;

@@ -117,7 +117,10 @@ struct EvictParams {
     Pages pages;
     int B, Hkv, D, Nk, n_keep, n_sink, n_recent;
     FastDiv div_hkv;
+    int parts;               // of a pair's rows (plan_evict), 0: one workgroup selects
+    unsigned *select_space;  // their counts and candidates, or null: one workgroup selects
 };
+long long plan_evict(EvictParams &p);  // bytes of workspace that the selection has use for
 hipError_t launch_evict(const EvictParams &p, hipStream_t stream);
 
 }  // namespace swaa

@@ -1,14 +1,14 @@
 // Eviction from a key/value cache by weight (gfx950): of the L rows of a sequence's KV head the first n_sink, the last n_recent and
 // the heaviest others stay, n_keep in all, and close up in their order; equal weights: the first rows stay.
 //
-// Two kernels:
-//   * Selection, a workgroup per (sequence, KV head): the weights as whole numbers of the same order; the least one that stays is
-//     found digit by digit (11, 11 and 10 bits) from counts in LDS, then every row's place from the counts of stayers before it.
-//     Writes `kept` and moves the weights.
+//   * Selection: the weights as whole numbers of the same order; the least one that stays is found digit by digit (11, 11 and 10
+//     bits) from counts in LDS, the last few candidates by ranking one against the others, then every row's place from the counts of
+//     stayers before it.  A workgroup to a (sequence, KV head) pair; long sequences of few pairs are shared out, in three steps.
 //   * Moves of K and V in place.  A row only ever moves down, so a workgroup that goes through the kept rows from the first on,
 //     reads a block of rows, waits until all its reads are done and only then writes them overwrites nothing that is still
 //     wanted.  Different columns of the rows do not meet: a workgroup takes a slice of a few bytes of every row, of K or of V, of
-//     one head.
+//     one head; the weights are one more.  Where half the rows leave or more, those that come from behind the first n_keep are left
+//     to a kernel of their own behind it, in any order: nothing is written where they stand.
 // Bound by memory: each row that moves is read and written once.
 #include "swaa_cache_ops.h"
 
@@ -21,6 +21,7 @@ constexpr int kSegment = 256;              // rows of a wave's step, four to a l
 constexpr int kStep = kSWaves * kSegment;  // rows of a workgroup's step
 constexpr int kBins = 2048, kDigitBits = 11;
 constexpr int kCopies = 4;                 // of the bins, side by side: lanes of equal weights seldom meet in one, nor in a bank
+constexpr int kMaxSteps = 8;               // of a round
 constexpr int kFew = 256;                  // candidates that are ranked one against the other
 
 // Rows as whole numbers that the heaviest ones have the largest of: a weight's bits in its order (-0 is 0, everything that is not a
@@ -32,6 +33,13 @@ __device__ __forceinline__ unsigned order_of(unsigned bits) {
     if (bits == 0x80000000u) bits = 0;
     return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
 }
+
+// What a selecting workgroup has in LDS.
+struct SelectLds {
+    __attribute__((aligned(16))) unsigned bins[kBins * kCopies];  // (or candidates, when the bins are done with)
+    unsigned scratch[kSWaves], scratch2[kSWaves], found[4];
+    unsigned heavier[kMaxSteps * kSWaves], equal[kMaxSteps * kSWaves];
+};
 
 // Exclusive sum over the workgroup's threads of x; `all`: of all of them.  Callers have a barrier between two calls.
 __device__ __forceinline__ unsigned block_exclusive(unsigned x, unsigned *scratch, unsigned &all) {
@@ -45,72 +53,85 @@ __device__ __forceinline__ unsigned block_exclusive(unsigned x, unsigned *scratc
     return before + incl - x;
 }
 
-// kSteps: steps of a round, whose rows' orders are in registers; longer sequences take several rounds and read their weights once
-// more for each look at them.
-template <int kSteps>
-__global__ __launch_bounds__(kSThreads) void swaa_evict_select_kernel(const EvictParams p) {
-    constexpr int kRound = kSteps * kStep;
-    __shared__ __attribute__((aligned(16))) unsigned bins[kBins * kCopies];
-    __shared__ unsigned scratch[kSWaves], scratch2[kSWaves], found[4];
-    __shared__ unsigned heavier[kSteps * kSWaves], equal[kSteps * kSWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const unsigned pair = blockIdx.x, b = fastdiv(pair, p.div_hkv), kvh = pair - b * (unsigned)p.Hkv;
-    const int n = p.seq_lens ? max(min(p.seq_lens[b], p.Nk), 0) : p.Nk;
-    int *kept = p.kept + (long long)pair * p.n_keep;
-    if (n <= p.n_keep) {
-        for (int i = tid; i < p.n_keep; i += kSThreads) kept[i] = i < n ? i : -1;
-        return;
+// A (sequence, KV head) pair that is longer than n_keep rows; false: one that keeps all it has (`kept` says so, if `says`).
+struct Head {
+    int n, lo, hi;  // rows lo .. hi - 1 are judged
+    int *kept;
+    __amdgpu_buffer_rsrc_t words;  // its weights (a buffer of n words: what is read behind them is 0, without a branch around the read)
+};
+__device__ __forceinline__ bool head_of(const EvictParams &p, unsigned pair, bool says, Head &h) {
+    const unsigned b = fastdiv(pair, p.div_hkv), kvh = pair - b * (unsigned)p.Hkv;
+    h.n = p.seq_lens ? max(min(p.seq_lens[b], p.Nk), 0) : p.Nk;
+    h.kept = p.kept + (long long)pair * p.n_keep;
+    if (h.n <= p.n_keep) {
+        if (says)
+            for (int i = threadIdx.x; i < p.n_keep; i += kSThreads) h.kept[i] = i < h.n ? i : -1;
+        return false;
     }
-    // (a buffer of n words: what is read behind them is 0, without a branch around the read)
-    const __amdgpu_buffer_rsrc_t words = __builtin_amdgcn_make_buffer_rsrc(p.weights + b * p.w_sb + kvh * p.w_sh, 0, 4 * n, 0x00027000);
-    const int lo = p.n_sink, hi = n - p.n_recent, rounds = (n + kRound - 1) / kRound;
+    h.lo = p.n_sink;
+    h.hi = h.n - p.n_recent;
+    h.words = __builtin_amdgcn_make_buffer_rsrc(p.weights + b * p.w_sb + kvh * p.w_sh, 0, 4 * h.n, 0x00027000);
+    return true;
+}
 
-    // element e (0 .. 3) of step s of a round: row first_of(round, s) + 64 e + lane
-    unsigned order[kSteps][4];
-    auto first_of = [&](int round, int s) { return round * kRound + s * kStep + wave * kSegment; };
-    auto load_round = [&](int round) __attribute__((always_inline)) {
-        int l = lane;
-        asm volatile("" : "+v"(l));  // (what depends on it is worked out here: kept from one look to the next it would need the registers)
+// Orders of kSteps steps of rows from row `begin` on: element e (0 .. 3) of step s is row first_row(begin, s) + 64 e + lane.
+__device__ __forceinline__ int first_row(int begin, int s) { return begin + s * kStep + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * kSegment; }
+template <int kSteps>
+__device__ __forceinline__ void load_orders(const Head &h, int begin, unsigned (&order)[kSteps][4]) {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));  // (what depends on it is worked out here: kept from one look to the next it would need the registers)
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
+    for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) order[s][e] = __builtin_amdgcn_raw_buffer_load_b32(words, 4 * (first_of(round, s) + 64 * e + l), 0, 0);
+        for (int e = 0; e < 4; ++e) order[s][e] = __builtin_amdgcn_raw_buffer_load_b32(h.words, 4 * (first_row(begin, s) + 64 * e + lane), 0, 0);
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int first = first_of(round, s);
+    for (int s = 0; s < kSteps; ++s) {
+        const int first = first_row(begin, s);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) order[s][e] = order_of(order[s][e]);
-            if (first < lo || first + kSegment > hi) {
+        for (int e = 0; e < 4; ++e) order[s][e] = order_of(order[s][e]);
+        if (first < h.lo || first + kSegment > h.hi) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = first + 64 * e + l;
-                    order[s][e] = i >= n ? 0u : i < lo || i >= hi ? kPinned : order[s][e];
-                }
+            for (int e = 0; e < 4; ++e) {
+                const int i = first + 64 * e + lane;
+                order[s][e] = i >= h.n ? 0u : i < h.lo || i >= h.hi ? kPinned : order[s][e];
             }
         }
-    };
-    // f(order) for every row
-    auto look = [&](auto f) __attribute__((always_inline)) {
-        for (int round = 0; round < rounds; ++round) {
-            if (rounds > 1) load_round(round);
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                if (first_of(round, s) >= n) break;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f(order[s][e]);
-            }
-        }
-    };
-    load_round(0);
+    }
+}
 
-    // ---- the least order that stays, from its highest bits down, until few rows have those
-    unsigned prefix = 0, mask = 0, left = (unsigned)p.n_keep;  // `left`: how many of those with the prefix stay
-    for (int shift = 32 - kDigitBits, width = kDigitBits; mask != ~0u;) {
-        static_assert(kCopies == 4 && kBins == 2 * kSThreads, "");
-        u32x4 *const four = reinterpret_cast<u32x4 *>(bins);
-        four[tid] = four[tid + kSThreads] = u32x4{0, 0, 0, 0};
-        __syncthreads();
-        unsigned *const mine = bins + lane % kCopies;
+// Thread t has the counts of bins 2047 - 2 t and the one below: finds the bin that holds the left-th from above.  found: the bin,
+// how many of its own stay, how many it has, 0.
+__device__ __forceinline__ void find_bin(const unsigned (&c)[2], unsigned left, SelectLds &lds) {
+    unsigned all;
+    const unsigned before = block_exclusive(c[0] + c[1], lds.scratch, all);
+    if (before < left && left <= before + c[0] + c[1]) {
+        const bool first = left <= before + c[0];
+        lds.found[0] = kBins - 1 - 2 * threadIdx.x - (first ? 0 : 1);
+        lds.found[1] = left - before - (first ? 0 : c[0]);
+        lds.found[2] = first ? c[0] : c[1];
+        lds.found[3] = 0;
+    }
+    __syncthreads();
+}
+__device__ __forceinline__ void clear_bins(SelectLds &lds) {
+    static_assert(kCopies == 4 && kBins == 2 * kSThreads, "");
+    u32x4 *const four = reinterpret_cast<u32x4 *>(lds.bins);
+    four[threadIdx.x] = four[threadIdx.x + kSThreads] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+}
+__device__ __forceinline__ unsigned bin_count(const SelectLds &lds, int bin) {
+    const u32x4 copies = reinterpret_cast<const u32x4 *>(lds.bins)[bin];
+    return (copies[0] + copies[1]) + (copies[2] + copies[3]);
+}
+
+// The least order that stays: `left` of those with the bits `prefix` under `mask` do, the digit at `shift` is the next to be looked at.
+// look(f) calls f(order) for all of a thread's rows.  On return prefix is that order, left how many of its equals stay.
+template <typename Look>
+__device__ __forceinline__ void find_least(Look look, unsigned &prefix, unsigned mask, unsigned &left, int shift, SelectLds &lds) {
+    const int tid = threadIdx.x;
+    while (mask != ~0u) {
+        clear_bins(lds);
+        unsigned *const mine = lds.bins + tid % kCopies;
         if (mask == 0)
             look([&](unsigned u) { atomicAdd(&mine[(u >> (32 - kDigitBits)) * kCopies], 1u); });
         else
@@ -118,32 +139,17 @@ __global__ __launch_bounds__(kSThreads) void swaa_evict_select_kernel(const Evic
                 if ((u & mask) == prefix) atomicAdd(&mine[((u >> shift) & (kBins - 1)) * kCopies], 1u);  // (the last digit has ten bits: the eleventh is the prefix's)
             });
         __syncthreads();
-        // thread t: bins 2047 - 2 t and the one below, the highest first
-        unsigned c[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const u32x4 copies = four[kBins - 1 - 2 * tid - k];
-            c[k] = (copies[0] + copies[1]) + (copies[2] + copies[3]);
-        }
-        unsigned all;
-        const unsigned before = block_exclusive(c[0] + c[1], scratch, all);
-        if (before < left && left <= before + c[0] + c[1]) {
-            const bool first = left <= before + c[0];
-            found[0] = kBins - 1 - 2 * tid - (first ? 0 : 1);
-            found[1] = left - before - (first ? 0 : c[0]);
-            found[2] = first ? c[0] : c[1];
-            found[3] = 0;
-        }
-        __syncthreads();
-        prefix |= found[0] << shift;
-        mask |= ((1u << width) - 1) << shift;
-        left = found[1];
-        const unsigned candidates = found[2];
+        const unsigned c[2] = {bin_count(lds, kBins - 1 - 2 * tid), bin_count(lds, kBins - 2 - 2 * tid)};
+        find_bin(c, left, lds);
+        prefix |= lds.found[0] << shift;
+        mask |= ((1u << kDigitBits) - 1) << shift;
+        left = lds.found[1];
+        const unsigned candidates = lds.found[2];
         if (candidates <= (unsigned)kFew && mask != ~0u) {
             // each of them against all others
-            unsigned *const few = bins;
+            unsigned *const few = lds.bins;
             look([&](unsigned u) {
-                if ((u & mask) == prefix) few[atomicAdd(&found[3], 1u)] = u;
+                if ((u & mask) == prefix) few[atomicAdd(&lds.found[3], 1u)] = u;
             });
             __syncthreads();
             if (tid < (int)candidates) {
@@ -154,73 +160,204 @@ __global__ __launch_bounds__(kSThreads) void swaa_evict_select_kernel(const Evic
                     same += few[i] == u;
                 }
                 if (above < left && left <= above + same) {  // (every thread that holds it says the same)
-                    found[0] = u;
-                    found[1] = left - above;
+                    lds.found[0] = u;
+                    lds.found[1] = left - above;
                 }
             }
             __syncthreads();
-            prefix = found[0];
-            left = found[1];
+            prefix = lds.found[0];
+            left = lds.found[1];
             mask = ~0u;
         }
-        width = shift < kDigitBits ? shift : kDigitBits;
-        shift -= width;
+        shift = shift > kDigitBits ? shift - kDigitBits : 0;
     }
+}
 
-    // ---- places: the heavier rows stay, and the first `left` of the equal ones
-    unsigned base_heavier = 0, base_equal = 0;
-    for (int round = 0; round < rounds; ++round) {
-        if (rounds > 1) load_round(round);
+// Places of the rows that stay among those from row `begin` on: the heavier ones do, and the first `left` of the equal ones.  base_*: of
+// the rows before them.
+template <int kSteps>
+__device__ __forceinline__ void put_rows(const Head &h, int begin, const unsigned (&order)[kSteps][4], unsigned prefix, unsigned left,
+                                         unsigned &base_heavier, unsigned &base_equal, SelectLds &lds) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            unsigned nh = 0, ne = 0;
-            if (first_of(round, s) < n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    nh += __popcll(__ballot(order[s][e] > prefix));
-                    ne += __popcll(__ballot(order[s][e] == prefix));
-                }
-            if (lane == 0) {
-                heavier[s * kSWaves + wave] = nh;
-                equal[s * kSWaves + wave] = ne;
-            }
-        }
-        __syncthreads();
-        // (the round's segments: their sums by the first threads)
-        const bool has = tid < kSteps * kSWaves;
-        unsigned all_heavier, all_equal;
-        const unsigned eh = block_exclusive(has ? heavier[tid] : 0u, scratch, all_heavier);
-        const unsigned ee = block_exclusive(has ? equal[tid] : 0u, scratch2, all_equal);
-        if (has) {
-            heavier[tid] = eh;
-            equal[tid] = ee;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int first = first_of(round, s);
-            if (first >= n) break;
-            unsigned h = base_heavier + heavier[s * kSWaves + wave], q = base_equal + equal[s * kSWaves + wave];
+    for (int s = 0; s < kSteps; ++s) {
+        unsigned nh = 0, ne = 0;
+        if (first_row(begin, s) < h.n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const unsigned u = order[s][e];
-                const unsigned long long bh = __ballot(u > prefix), bq = __ballot(u == prefix);
-                unsigned place = h + min(q, left) + __builtin_amdgcn_mbcnt_hi((unsigned)(bh >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)bh, 0u));
-                bool stays = u > prefix;
-                if (bq) {
-                    const unsigned my_q = q + __builtin_amdgcn_mbcnt_hi((unsigned)(bq >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)bq, 0u));
-                    place += min(my_q, left) - min(q, left);
-                    stays = stays || (u == prefix && my_q < left);
-                    q += __popcll(bq);
-                }
-                if (stays) kept[place] = first + 64 * e + lane;
-                h += __popcll(bh);
+                nh += __popcll(__ballot(order[s][e] > prefix));
+                ne += __popcll(__ballot(order[s][e] == prefix));
+            }
+        if (lane == 0) {
+            lds.heavier[s * kSWaves + wave] = nh;
+            lds.equal[s * kSWaves + wave] = ne;
+        }
+    }
+    __syncthreads();
+    // (the segments: their sums by the first threads)
+    const bool has = tid < kSteps * kSWaves;
+    unsigned all_heavier, all_equal;
+    const unsigned eh = block_exclusive(has ? lds.heavier[tid] : 0u, lds.scratch, all_heavier);
+    const unsigned ee = block_exclusive(has ? lds.equal[tid] : 0u, lds.scratch2, all_equal);
+    if (has) {
+        lds.heavier[tid] = eh;
+        lds.equal[tid] = ee;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        const int first = first_row(begin, s);
+        if (first >= h.n) break;
+        unsigned before = base_heavier + lds.heavier[s * kSWaves + wave], q = base_equal + lds.equal[s * kSWaves + wave];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned u = order[s][e];
+            const unsigned long long bh = __ballot(u > prefix), bq = __ballot(u == prefix);
+            unsigned place = before + min(q, left) + __builtin_amdgcn_mbcnt_hi((unsigned)(bh >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)bh, 0u));
+            bool stays = u > prefix;
+            if (bq) {
+                const unsigned my_q = q + __builtin_amdgcn_mbcnt_hi((unsigned)(bq >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)bq, 0u));
+                place += min(my_q, left) - min(q, left);
+                stays = stays || (u == prefix && my_q < left);
+                q += __popcll(bq);
+            }
+            if (stays) h.kept[place] = first + 64 * e + lane;
+            before += __popcll(bh);
+        }
+    }
+    base_heavier += all_heavier;
+    base_equal += all_equal;
+}
+
+// One workgroup to a pair.  kSteps: steps of a round, whose rows' orders are in registers; longer sequences take several rounds and
+// read their weights once more for each look at them.
+template <int kSteps>
+__global__ __launch_bounds__(kSThreads) void swaa_evict_select_kernel(const EvictParams p) {
+    static_assert(kSteps <= kMaxSteps, "");
+    __shared__ SelectLds lds;
+    Head h;
+    if (!head_of(p, blockIdx.x, true, h)) return;
+    const int rounds = (h.n + kSteps * kStep - 1) / (kSteps * kStep);
+    unsigned order[kSteps][4];
+    auto look = [&](auto f) __attribute__((always_inline)) {
+        for (int round = 0; round < rounds; ++round) {
+            if (rounds > 1) load_orders<kSteps>(h, round * kSteps * kStep, order);
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                if (first_row(round * kSteps * kStep, s) >= h.n) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f(order[s][e]);
             }
         }
-        base_heavier += all_heavier;
-        base_equal += all_equal;
+    };
+    load_orders<kSteps>(h, 0, order);
+    unsigned prefix = 0, left = (unsigned)p.n_keep, base_heavier = 0, base_equal = 0;
+    find_least(look, prefix, 0u, left, 32 - kDigitBits, lds);
+    for (int round = 0; round < rounds; ++round) {
+        if (rounds > 1) load_orders<kSteps>(h, round * kSteps * kStep, order);
+        put_rows<kSteps>(h, round * kSteps * kStep, order, prefix, left, base_heavier, base_equal, lds);
         __syncthreads();
     }
+}
+
+// ---- long sequences of few pairs: a workgroup to every kPartRows rows of a pair.  Counts of the first digit, then the rows of the digit
+// that the least one has (the candidates) one part behind the other, then its other digits from those and the part's places. ----
+constexpr int kPartSteps = 2, kPartRows = kPartSteps * kStep;
+struct PartSpace {
+    unsigned *counts, *candidates;  // [parts][bins], [Nk]
+};
+__device__ __forceinline__ PartSpace part_space(const EvictParams &p, unsigned pair) {
+    unsigned *const at = p.select_space + (long long)pair * ((long long)p.parts * kBins + p.Nk + p.Nk % 2);  // (pairs of counts are read at once)
+    return {at, at + (long long)p.parts * kBins};
+}
+// The digit of the least row that stays (found[0], as find_bin leaves it) and how many rows of the parts before `part` are above it
+// and in it.
+__device__ __forceinline__ void first_digit(const EvictParams &p, const PartSpace &space, int part, int parts, SelectLds &lds, unsigned &above, unsigned &in) {
+    const int tid = threadIdx.x;
+    unsigned c[2] = {0, 0}, mine[2] = {0, 0};  // of all parts, and of those before
+    for (int i = 0; i < parts; ++i) {
+        const uint2 two = *reinterpret_cast<const uint2 *>(space.counts + (long long)i * kBins + kBins - 2 - 2 * tid);
+        c[0] += two.y;
+        c[1] += two.x;
+        mine[0] += i < part ? two.y : 0u;
+        mine[1] += i < part ? two.x : 0u;
+    }
+    find_bin(c, (unsigned)p.n_keep, lds);
+    const unsigned bin = lds.found[0];
+    unsigned sums[2] = {0, 0};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const unsigned of = (unsigned)(kBins - 1 - 2 * tid - k);
+        sums[0] += of > bin ? mine[k] : 0u;
+        sums[1] += of == bin ? mine[k] : 0u;
+    }
+    block_exclusive(sums[0], lds.scratch2, above);
+    __syncthreads();
+    block_exclusive(sums[1], lds.scratch, in);
+    __syncthreads();
+}
+__global__ __launch_bounds__(kSThreads) void swaa_evict_count_kernel(const EvictParams p) {
+    __shared__ SelectLds lds;
+    const unsigned pairs = (unsigned)(p.B * p.Hkv), pair = blockIdx.x % pairs, part = blockIdx.x / pairs;
+    Head h;
+    if (!head_of(p, pair, part == 0, h) || (int)part * kPartRows >= h.n) return;
+    unsigned order[kPartSteps][4];
+    load_orders<kPartSteps>(h, (int)part * kPartRows, order);
+    clear_bins(lds);
+#pragma unroll
+    for (int s = 0; s < kPartSteps; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) atomicAdd(&lds.bins[(order[s][e] >> (32 - kDigitBits)) * kCopies + threadIdx.x % kCopies], 1u);
+    __syncthreads();
+    unsigned *const out = part_space(p, pair).counts + (long long)part * kBins;
+    for (int i = threadIdx.x; i < kBins; i += kSThreads) out[i] = bin_count(lds, i);
+}
+__global__ __launch_bounds__(kSThreads) void swaa_evict_gather_kernel(const EvictParams p) {
+    __shared__ SelectLds lds;
+    const unsigned pairs = (unsigned)(p.B * p.Hkv), pair = blockIdx.x % pairs, part = blockIdx.x / pairs;
+    Head h;
+    if (!head_of(p, pair, false, h) || (int)part * kPartRows >= h.n) return;
+    unsigned order[kPartSteps][4], above, in;
+    load_orders<kPartSteps>(h, (int)part * kPartRows, order);
+    const PartSpace space = part_space(p, pair);
+    first_digit(p, space, (int)part, (h.n + kPartRows - 1) / kPartRows, lds, above, in);
+    const unsigned bin = lds.found[0];  // (found[3] is 0: the part's candidates so far)
+    unsigned *const out = space.candidates + in;
+#pragma unroll
+    for (int s = 0; s < kPartSteps; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (order[s][e] >> (32 - kDigitBits) == bin) out[atomicAdd(&lds.found[3], 1u)] = order[s][e];
+}
+__global__ __launch_bounds__(kSThreads) void swaa_evict_put_kernel(const EvictParams p) {
+    __shared__ SelectLds lds;
+    const unsigned pairs = (unsigned)(p.B * p.Hkv), pair = blockIdx.x % pairs, part = blockIdx.x / pairs;
+    Head h;
+    if (!head_of(p, pair, false, h) || (int)part * kPartRows >= h.n) return;
+    unsigned order[kPartSteps][4], above, in;
+    load_orders<kPartSteps>(h, (int)part * kPartRows, order);
+    const PartSpace space = part_space(p, pair);
+    first_digit(p, space, (int)part, (h.n + kPartRows - 1) / kPartRows, lds, above, in);
+    const unsigned bin = lds.found[0], n = lds.found[2];
+    unsigned prefix = bin << (32 - kDigitBits), left = lds.found[1];
+    __syncthreads();  // (found is read)
+    auto look = [&](auto f) {
+        for (unsigned i = threadIdx.x; i < n; i += kSThreads) f(space.candidates[i]);
+    };
+    find_least(look, prefix, ((1u << kDigitBits) - 1) << (32 - kDigitBits), left, 32 - 2 * kDigitBits, lds);
+    // candidates of the parts before this one: the heavier, the equal
+    unsigned heavier = 0, equal = 0;
+    for (unsigned i = threadIdx.x; i < in; i += kSThreads) {
+        heavier += space.candidates[i] > prefix;
+        equal += space.candidates[i] == prefix;
+    }
+    unsigned base_heavier, base_equal;
+    __syncthreads();
+    block_exclusive(heavier, lds.scratch, base_heavier);
+    block_exclusive(equal, lds.scratch2, base_equal);
+    base_heavier += above;
+    __syncthreads();
+    put_rows<kPartSteps>(h, (int)part * kPartRows, order, prefix, left, base_heavier, base_equal, lds);
 }
 
 constexpr int kMThreads = 1024;
@@ -378,16 +515,29 @@ void move_far(const EvictParams &p, hipStream_t stream) {
 
 }  // namespace
 
+// Sequences of more rows than a few steps, in so few pairs that a workgroup each would leave most of the chip idle.
+long long plan_evict(EvictParams &p) {
+    const long long pairs = (long long)p.B * p.Hkv;
+    p.parts = p.Nk > 4 * kStep && pairs <= 64 ? (p.Nk + kPartRows - 1) / kPartRows : 0;
+    return p.parts ? pairs * ((long long)p.parts * kBins + p.Nk + p.Nk % 2) * (long long)sizeof(unsigned) : 0;
+}
+
 hipError_t launch_evict(const EvictParams &params, hipStream_t stream) {
     EvictParams p = params;
     const bool in_place = p.new_lens && p.new_lens == p.seq_lens;
     if (in_place) p.new_lens = nullptr;
-    if (p.Nk <= kStep)
+    if (p.select_space) {
+        const dim3 wgs((unsigned)(p.B * p.Hkv) * (unsigned)p.parts);
+        swaa_evict_count_kernel<<<wgs, dim3(kSThreads), 0, stream>>>(p);
+        swaa_evict_gather_kernel<<<wgs, dim3(kSThreads), 0, stream>>>(p);
+        swaa_evict_put_kernel<<<wgs, dim3(kSThreads), 0, stream>>>(p);
+    } else if (p.Nk <= kStep) {
         select<1>(p, stream);
-    else if (p.Nk <= 4 * kStep)
+    } else if (p.Nk <= 4 * kStep) {
         select<4>(p, stream);
-    else
-        select<16>(p, stream);
+    } else {
+        select<8>(p, stream);
+    }
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     // Half the rows leave or more: most that stay come from behind the first n_keep.

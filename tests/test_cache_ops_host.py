@@ -124,9 +124,20 @@ def test_evict_refusals(status, kw):
     assert evict(**kw) == getattr(binding, "SWAA_ERR_" + status)
 
 
+def test_evict_workspace():
+    need = binding.swaa_cache_evict_workspace_bytes(2, 2, 100000, 128)
+    long = dict(Nk=100000, weights_stride_b=200000, weights_stride_h=100000, k=rows(2, 100000, 128), v=rows(2, 100000, 128))
+    assert need > 0 and evict(workspace=P, workspace_bytes=need - 1, **long) == binding.SWAA_ERR_WORKSPACE
+    assert evict(workspace=P + 8, workspace_bytes=need, **long) == binding.SWAA_ERR_WORKSPACE
+    assert binding.swaa_cache_evict_workspace_bytes(64, 8, 131072, 128) == binding.swaa_cache_evict_workspace_bytes(1, 8, 4096, 128) == 0
+    for bad in ((0, 2, 100, 128), (1, 2, 0, 128), (1, 2, 100, 100), (1, 2, (1 << 28) + 1, 128)):
+        with pytest.raises(binding.SwaaError):
+            binding.swaa_cache_evict_workspace_bytes(*bad)
+
+
 def test_a_missing_argument_block():
     for name in ("swaa_qk_norm_rope", "swaa_qk_norm_rope_bwd", "swaa_attn_key_weights", "swaa_cache_evict",
-                 "swaa_qk_norm_rope_bwd_workspace_bytes", "swaa_attn_key_weights_workspace_bytes"):
+                 "swaa_qk_norm_rope_bwd_workspace_bytes", "swaa_attn_key_weights_workspace_bytes", "swaa_cache_evict_workspace_bytes"):
         assert getattr(binding.load_library(), name)(None) == binding.SWAA_ERR_NULL
 
 

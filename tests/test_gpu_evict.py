@@ -117,3 +117,52 @@ def test_pages_outside_the_cache():
         named = set(good.flatten().tolist())
         strangers = [p for p in range(pages) if p not in named] + [int(good[0, 0]), int(good[0, 3])]  # (in no table now)
         assert torch.equal(data[strangers], c.data[strangers])
+
+
+def select_only(weights, lens, n_keep, n_sink, n_recent, space):
+    """The C call on a cache of one byte-sized row type, with a workspace or without; kept rows and weights."""
+    B, H, N = weights.shape
+    k = torch.zeros(B, H, N, 32, dtype=torch.float16, device="cuda")
+    w, kept = weights.cuda(), torch.full((B, H, n_keep), -7, dtype=torch.int32, device="cuda")
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    a = binding.SwaaEvictArgs()
+    a.k = a.v = binding.SwaaTensor(k.data_ptr(), H * N * 32, N * 32, 32)
+    a.weights, a.weights_stride_b, a.weights_stride_h = w.data_ptr(), H * N, N
+    a.kept, a.seq_lens, a.B, a.Hkv, a.D, a.Nk = kept.data_ptr(), seq.data_ptr(), B, H, 32, N
+    a.n_keep, a.n_sink, a.n_recent, a.stream = n_keep, n_sink, n_recent, torch.cuda.current_stream().cuda_stream
+    need = binding.swaa_cache_evict_workspace_bytes(B, H, N, 32)
+    if space:
+        room = torch.full((need + 64,), 0xee, dtype=torch.uint8, device="cuda")
+        a.workspace, a.workspace_bytes = room.data_ptr(), need
+    binding._call("swaa_cache_evict", a)
+    torch.cuda.synchronize()
+    if space:
+        assert (room[need:] == 0xee).all()
+    return kept.cpu(), w.cpu(), need
+
+
+@pytest.mark.parametrize("ties", [0, 5, 1])
+@pytest.mark.parametrize("lens", [[16385, 3, 16384], [40000, 20001], [100001]])
+def test_long_sequences_shared_out_and_not(lens, ties):
+    gen = torch.Generator().manual_seed(lens[0] + ties)
+    N, n_keep, n_sink, n_recent = max(lens), max(lens) // 3, 4, 1000
+    w = random_weights(len(lens), 2, N, gen, ties)
+    shared, w1, need = select_only(w, lens, n_keep, n_sink, n_recent, True)
+    alone, w2, _ = select_only(w, lens, n_keep, n_sink, n_recent, False)
+    assert need > 0 and torch.equal(shared, alone) and torch.equal(w1, w2)
+    for b, n in enumerate(lens):
+        for g in range(2):
+            want = ref.evict(w[b, g, :n], n, n_keep, n_sink, n_recent)
+            assert shared[b, g].tolist() == want + [-1] * (n_keep - len(want))
+
+
+def test_many_long_sequences():
+    """More pairs than are shared out: a workgroup each, in rounds."""
+    gen = torch.Generator().manual_seed(70)
+    lens = [17000 + 41 * i for i in range(33)]
+    w = random_weights(33, 2, max(lens), gen)
+    kept, _, need = select_only(w, lens, 5000, 0, 7, True)
+    assert need == 0
+    for b in (0, 16, 32):
+        for g in range(2):
+            assert kept[b, g].tolist() == ref.evict(w[b, g, :lens[b]], lens[b], 5000, 0, 7)
