@@ -414,9 +414,10 @@ long long swaa_attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int N, int D, in
  *   k_out, v_out  the cache: Hkv heads of Nk rows (strided, packed or paged), of which the new tokens' are written; without a
  *                 cache (Nk = Nq, no seq_lens) the results' own rows, which may then be k and v themselves
  *   The sequences are those of swaa_attn_fwd_ex and swaa_attn_decode_ex: row r of sequence b is the token in row
- *   Nk_b - Nq_b + r of its cache, and row r of its q, k, v.  Fixed-length batches: Nq_b = Nq, Nk_b = seq_lens[b] clamped to
- *   [Nq, Nk] (seq_lens NULL: Nk).  Packed batches: both offsets given, as in swaa_fwd_args (total_rows_q too); seq_lens must be
- *   NULL.  Paged caches: as there, with pages of any size; a row whose page number lies outside the cache is not written.
+ *   Nk_b - Nq_b + r of its cache, and row r of its q, k, v.  Fixed-length batches: Nq_b = Nq, Nk_b = seq_lens[b] (NULL: Nk).
+ *   Packed batches: both offsets given, as in swaa_fwd_args (total_rows_q too); seq_lens must be NULL.  Paged caches: as there,
+ *   with pages of any size.  Keys and values whose row lies outside [0, Nk) (sequences of length 0 that pad a batch; a cache that is
+ *   full) or in a page whose number lies outside the cache are not written; their q_out is.
  *   positions     device ints, [B, Nq] contiguous or one per row of the packed tensors, or NULL: the row in the cache.  (They
  *                 differ behind an eviction: tokens have left the cache, positions go on.)
  *   q_weight, k_weight  device fp32 [D], or both NULL: no norm; eps finite and > 0 (not looked at without weights)
@@ -494,7 +495,8 @@ long long swaa_qk_norm_rope_bwd_workspace_bytes(const swaa_norm_rope_bwd_args *a
  * -infinity adds nothing; a key gets nothing from rows that do not see it, whatever the two hold.
  *
  *   q, k       read only; sequences, strides, alignment, head dimensions, dtype as in swaa_norm_rope_args (q its q, k its k_out);
- *              page numbers outside the cache are clamped to it
+ *              lengths are clamped to [0, Nk], page numbers to the cache; the rows of a fixed-length batch's sequence shorter
+ *              than Nq (padding) do not count
  *   lse        device fp32, rows contiguous, as in swaa_fwd_args
  *   weights    device fp32, weights[b * weights_stride_b + g * weights_stride_h + j], sequences one by one in packed batches, too
  *   decay      finite and >= 0

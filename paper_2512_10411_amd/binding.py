@@ -938,7 +938,8 @@ def swaa_qk_norm_rope(q, k, inv_freq=None, positions=None, q_weight=None, k_weig
     Without a cache the results are new contiguous tensors (q_out, k_out: others, q and k themselves among them).
     With one, k_out and v_out are the cache: [B, Hkv, Nk, D] views, packed [Hkv, Tk, D], or pages [num_pages, Hkv, page_size, D]
     with block_table and max_seqlen_k, as the attention calls take it; the call's tokens are the newest of seq_lens (int32 [B];
-    None: Nk) or of cu_seqlens_k, their own rows included.  Returns (q_out, k_out, v_out); v_out is None without v.
+    None: Nk) or of cu_seqlens_k, their own rows included; those whose row the cache does not have (a length of 0, or more than
+    Nk) are not written to it.  Returns (q_out, k_out, v_out); v_out is None without v.
     """
     tc = torch or _torch()
     if q_out is None and stream is None:

@@ -18,10 +18,11 @@ struct Rows {
 // The sequences of a call: fixed-length (cu_q null; seq_lens or Nk keys each) or packed.
 struct Sequences {
     const int *cu_q, *cu_k;   // B + 1 offsets each, or both null
-    const int *seq_lens;      // B lengths, clamped to [Nq, Nk], or null
+    const int *seq_lens;      // B lengths, or null
     int B, Nq, Nk;
 };
-// Query rows and keys of sequence b: its rows are the newest nq of its nk tokens.  Negative lengths count as none.
+// Query rows and keys of sequence b: its rows are the newest nq of its nk tokens.  Lengths are clamped to [0, Nk]; a fixed-length batch's
+// sequence shorter than its rows (padding) has no rows.
 __device__ __forceinline__ void sequence(const Sequences &s, int b, int &nq, int &nk) {
     nq = s.Nq;
     nk = s.Nk;
@@ -31,7 +32,8 @@ __device__ __forceinline__ void sequence(const Sequences &s, int b, int &nq, int
         nk = max(min(nk, s.Nk), 0);
         nq = min(nq, nk);
     } else if (s.seq_lens) {
-        nk = max(min(s.seq_lens[b], s.Nk), s.Nq);
+        nk = max(min(s.seq_lens[b], s.Nk), 0);
+        nq = nk < s.Nq ? 0 : s.Nq;
     }
 }
 

@@ -75,7 +75,7 @@ struct Token {
     int b, row;  // batch entry to take strides of, row along the tensors' row axis
     int pos;
     int of, at;  // its sequence and row in that one's cache
-    bool live;
+    bool live, cached;  // is there such a token, and has the cache its row?
 };
 __device__ __forceinline__ Token find_token(const NormRopeParams &p, long long slot) {
     Token t;
@@ -96,12 +96,18 @@ __device__ __forceinline__ Token find_token(const NormRopeParams &p, long long s
         b = (int)fastdiv((unsigned)mine, p.div_nq);
         r = mine - b * p.seq.Nq;
     }
-    sequence(p.seq, b, nq, nk);
+    if (p.seq.seq_lens) {  // (lengths as they are: rows outside the cache -- padding, or a cache that is full -- are not written)
+        nq = p.seq.Nq;
+        nk = p.seq.seq_lens[b];
+    } else {
+        sequence(p.seq, b, nq, nk);
+    }
     t.live = t.live && r >= 0 && r < nq;
     t.of = b;
     t.b = p.seq.cu_q ? 0 : b;
     t.row = r + (p.seq.cu_q ? p.seq.cu_q[b] : 0);
-    t.at = nk - nq + r;
+    t.at = (int)((unsigned)nk - (unsigned)nq + (unsigned)r);
+    t.cached = t.live && t.at >= 0 && t.at < p.seq.Nk;
     t.pos = !t.live ? 0 : !p.positions ? t.at : p.positions[p.seq.cu_q ? (long long)t.row : b * (long long)p.seq.Nq + r];
     return t;
 }
@@ -296,16 +302,16 @@ __global__ __launch_bounds__(kNThreads, 4) void swaa_norm_rope_kernel(const Norm
     }
     if (u_end <= k_first) return;
     const long long row0 = p.seq.cu_k && !p.pages.block_table ? p.seq.cu_k[t.of] : 0;
-    const int row = t.live ? t.at : 0;
+    const int row = t.cached ? t.at : 0;
     bool inside;
     if (k_begin < k_end) {
         const long long k_at = cache_row(p.pages, p.k_out, t.of, row0, row, p.seq.cu_k != nullptr, inside);
-        Heads k_out = heads_of(p.k_out, k_at, p.Hkv, k_first, live && inside);
+        Heads k_out = heads_of(p.k_out, k_at, p.Hkv, k_first, live && t.cached && inside);
         rows(k_in, k_out, k_begin, k_end, p.k_weight);
     }
     if (v_begin >= u_end) return;
     const long long v_at = cache_row(p.pages, p.v_out, t.of, row0, row, p.seq.cu_k != nullptr, inside);
-    Heads v_in = heads_of(p.v, t.b * p.v.sb + t.row * p.v.sn, p.Hkv, v_first, live), v_out = heads_of(p.v_out, v_at, p.Hkv, v_first, live && inside);
+    Heads v_in = heads_of(p.v, t.b * p.v.sb + t.row * p.v.sn, p.Hkv, v_first, live), v_out = heads_of(p.v_out, v_at, p.Hkv, v_first, live && t.cached && inside);
     for (int u = v_begin; u < u_end; u += kAhead) {
         load(v_in, u, u_end, raw);
 #pragma unroll

@@ -4,16 +4,14 @@ import math
 import torch
 
 
-def sequences(B, Nq, Nk, new=None, lens=None, seq_lens=None):
-    """[(rows, keys)] of a call: packed sequences (new, lens) or fixed-length ones."""
-    if new is not None:
-        out = []
-        for m, n in zip(new, lens):
-            m = max(min(m, Nq, n), 0)
-            n = max(min(n, Nk), 0)
-            out.append((min(m, n), n))
-        return out
-    return [(Nq, Nk if seq_lens is None else max(min(n, Nk), Nq)) for n in (seq_lens or [0] * B)]
+def sequences(Nq, Nk, new, lens):
+    """[(rows, keys)] of packed sequences."""
+    out = []
+    for m, n in zip(new, lens):
+        m = max(min(m, Nq, n), 0)
+        n = max(min(n, Nk), 0)
+        out.append((min(m, n), n))
+    return out
 
 
 def pairs_of(D, R, interleaved):

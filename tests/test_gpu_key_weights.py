@@ -105,7 +105,7 @@ def test_packed_batches(paged):
     lse = torch.full((Hq, sum(new)), float("nan"))  # (rows that do not count: whatever)
     old = torch.rand(B, Hkv, Nk, generator=gen)
     wants = []
-    for b, (m, n) in enumerate(ref.sequences(0, Nq, Nk, new, lens)):
+    for b, (m, n) in enumerate(ref.sequences(Nq, Nk, new, lens)):
         at = slice(int(cu_q[b]), int(cu_q[b]) + m)
         seen = ref.visible(m, n, window, n_sink, 10 ** 9)
         if m:
@@ -171,3 +171,28 @@ def test_against_the_64_bit_definition_on_many_rows():
     lse = ref.lse_of(q[0], k[0], scale, seen)[None].float()
     want, bound = ref.key_weights(q[0], k[0], lse[0], scale, seen)
     check(binding.swaa_attn_key_weights(q.cuda(), k.cuda(), lse.cuda(), window, n_sink, scale=scale)[0], want, bound, "many rows")
+
+
+def test_sequences_that_pad_a_batch():
+    """Lengths of 0, below the number of rows and beyond the cache: no rows, or as many keys as there are."""
+    gen = torch.Generator().manual_seed(51)
+    Hq, Hkv, D, Nq, Nk = 4, 2, 64, 3, 70
+    lens, held = [0, 2, -4, 70, 500, 3], [0, 2, 0, 70, 70, 3]
+    B = len(lens)
+    q, k = torch.randn(B, Hq, Nq, D, generator=gen).half(), torch.randn(B, Hkv, Nk, D, generator=gen).half()
+    lse, old = torch.full((B, Hq, Nq), float("nan")), torch.rand(B, Hkv, Nk, generator=gen)
+    wants = []
+    for b, n in enumerate(held):
+        m = Nq if n >= Nq else 0
+        seen = ref.visible(m, n, 10 ** 9, 0, 10 ** 9)
+        if m:
+            lse[b] = ref.lse_of(q[b], k[b, :, :n], 0.125, seen).float()
+        wants.append(ref.key_weights(q[b, :, :m], k[b, :, :n], lse[b, :, :m], 0.125, seen))
+    got = binding.swaa_attn_key_weights(q.cuda(), k.cuda(), lse.cuda(), 10 ** 9, 0, scale=0.125, weights=old.cuda(), decay=0.5,
+                                        seq_lens=torch.tensor(lens, dtype=torch.int32).cuda())
+    for b, (want, bound) in enumerate(wants):
+        n = held[b]
+        summed = want + 0.5 * old[b, :, :n].double()
+        if n:
+            check(got[b, :, :n], summed, bound + 2.0 ** -23 * (summed + want), f"length {lens[b]}")
+        assert torch.equal(got[b, :, n:].cpu(), old[b, :, n:])

@@ -96,7 +96,7 @@ def test_in_place():
 
 @pytest.mark.parametrize("page_size", [16, 4, 7, 1])
 @pytest.mark.parametrize("kind,B,Nq,Nk,lens,given", [
-    ("paged", 5, 1, 90, [1, 90, 17, 33, 64], True), ("paged", 3, 4, 60, [4, 2, 77], False), ("dense", 4, 1, 40, [40, 1, 7, 16], False),
+    ("paged", 5, 1, 90, [1, 90, 17, 33, 64], True), ("paged", 6, 4, 60, [4, 2, 77, 0, -5, 62], False), ("dense", 5, 1, 40, [40, 1, 7, 0, 41], False),
     ("rows", 2, 3, 50, None, True), ("paged", 70, 1, 20, list(range(1, 21)) * 3 + [20] * 10, True), ("dense", 1, 33, 33, None, False)])
 def test_new_tokens_go_into_the_cache(kind, B, Nq, Nk, lens, given, page_size):
     if kind != "paged" and page_size != 16:
@@ -118,13 +118,17 @@ def test_new_tokens_go_into_the_cache(kind, B, Nq, Nk, lens, given, page_size):
                                            max_seqlen_k=Nk if kind == "paged" else None)
     assert ko is kc.view and vo is vc.view
     want_k, want_v, size = kc.data.double(), vc.data.clone(), torch.zeros_like(kc.data, dtype=torch.float64)
-    for b, (m, n) in enumerate(ref.sequences(B, Nq, Nk, seq_lens=lens)):
-        at = torch.arange(n - m, n) if pos is None else pos[b]
+    for b, n in enumerate(lens or [Nk] * B):
+        rows = torch.arange(n - Nq, n)
+        at = rows if pos is None else pos[b]
         close(qo[b], *ref.norm_rope(parts[0][b], qw, at, inv, 1e-6, False), torch.bfloat16, f"q of {b}")
         y, s = ref.norm_rope(parts[1][b], kw, at, inv, 1e-6, False)
-        kc.put(want_k, b, n - m, y)
-        kc.put(size, b, n - m, s)
-        vc.put(want_v, b, n - m, parts[2][b])
+        there = (rows >= 0) & (rows < Nk)  # (what the cache has no row for is not written)
+        if there.any():
+            first = int(rows[there][0])
+            kc.put(want_k, b, first, y[:, there])
+            kc.put(size, b, first, s[:, there])
+            vc.put(want_v, b, first, parts[2][b][:, there])
     close(kc.gpu, want_k, size, torch.bfloat16, "cache")  # (rows of others: size 0, and what stood there)
     untouched = size.sum(-1) == 0
     assert torch.equal(kc.gpu.cpu()[untouched], kc.data[untouched])
@@ -162,7 +166,7 @@ def test_packed_batches(paged, stated):
     binding.swaa_qk_norm_rope(gq, gk, inv.cuda(), v=gv, q_out=qo, k_out=kg, v_out=vg, cu_seqlens_q=cu_q.cuda(), cu_seqlens_k=cu_k.cuda(),
                               max_seqlen_q=Nq, max_seqlen_k=Nk, block_table=kc.table if paged else None, total_rows_q=total)
     want_q, size_q, want_k, size_k, want_v = q_start.double(), torch.zeros(Hq, T, D, dtype=torch.float64), kd.double(), torch.zeros_like(kd, dtype=torch.float64), vd.clone()
-    for b, (m, n) in enumerate(ref.sequences(0, Nq, Nk, new, lens)):
+    for b, (m, n) in enumerate(ref.sequences(Nq, Nk, new, lens)):
         if stated == "fewer" and b == 6:
             continue
         rows = slice(int(cu_q[b]), int(cu_q[b]) + m)
