@@ -52,7 +52,7 @@ const char *swaa_status_string(int status) {
         case SWAA_OK: return "ok";
         case SWAA_ERR_NULL: return "null pointer argument";
         case SWAA_ERR_SHAPE: return "size, window, sink count, prompt length or scale out of range";
-        case SWAA_ERR_UNSUPPORTED: return "unsupported head dimension or element type (forward: multiples of 32 up to 256; decode: 128; backward: 64 and 128)";
+        case SWAA_ERR_UNSUPPORTED: return "unsupported head dimension or element type (forward: multiples of 32 up to 256; decode: 128; backward: 64 and 128; norms and cache: multiples of 32 up to 256, rotated dimensions multiples of 16)";
         case SWAA_ERR_ALIGN: return "pointer not 16-byte aligned";
         case SWAA_ERR_LAUNCH: return "HIP launch failed";
         case SWAA_ERR_WORKSPACE: return "workspace missing, misaligned or too small (or the call needs more scratch than the static array holds)";
@@ -642,7 +642,8 @@ int evict_plan(const swaa_evict_args *a, swaa::EvictParams &p, long long &ws_byt
     const int rc = check_heads(a->B, a->Hkv, a->Hkv, a->D);
     if (rc != SWAA_OK) return rc;
     if (a->Nk < 1 || a->Nk > (1 << 28)) return SWAA_ERR_SHAPE;  // (weights of a head below 2 GiB)
-    if ((long long)a->B * a->Hkv > 0x7fffffffLL / 256) return SWAA_ERR_SHAPE;
+    // (a launch has fewer than 2^32 threads: what cannot be moved is not selected either)
+    if ((long long)a->B * a->Hkv * (1 + a->D / 8) >= 1LL << 22) return SWAA_ERR_SHAPE;
     p.B = a->B;
     p.Hkv = a->Hkv;
     p.D = a->D;

@@ -9,7 +9,9 @@
 //     wanted.  Different columns of the rows do not meet: a workgroup takes a slice of a few bytes of every row, of K or of V, of
 //     one head; the weights are one more.  Where half the rows leave or more, those that come from behind the first n_keep are left
 //     to a kernel of their own behind it, in any order: nothing is written where they stand.
-// Bound by memory: each row that moves is read and written once.
+// Bound by memory: each row that moves is read and written once.  16 sequences of 900 to 1152 rows, 8 heads of 128, cut to 1024:
+// 31 us, of it 7 for the selection; one of 65536 cut to 16384: 64 us, of it 20 for the selection, 15 for rows from near by, in order,
+// and 22 for those from far (100 MB that come and go, 4.6 TB/s).
 #include "swaa_cache_ops.h"
 
 namespace swaa {
@@ -515,10 +517,12 @@ void move_far(const EvictParams &p, hipStream_t stream) {
 
 }  // namespace
 
-// Sequences of more rows than a few steps, in so few pairs that a workgroup each would leave most of the chip idle.
+// Shared out: pairs longer than one workgroup holds in a round, so few of them that a workgroup each would leave most of the chip idle
+// (call with the moves, a workgroup each against shared out: 8 pairs of 65536 rows to 16384 76.2 -> 52.0 us, 64 of 40000 to 2000
+// 74.0 -> 55.6, 96 of those 97.6 -> 79.8, 128 of 65536 to 16384 537 and 542; 8 of 20000 to 5000 29.8 -> 32.4).
 long long plan_evict(EvictParams &p) {
     const long long pairs = (long long)p.B * p.Hkv;
-    p.parts = p.Nk > 4 * kStep && pairs <= 64 ? (p.Nk + kPartRows - 1) / kPartRows : 0;
+    p.parts = p.Nk > kMaxSteps * kStep && pairs <= 96 ? (p.Nk + kPartRows - 1) / kPartRows : 0;
     return p.parts ? pairs * ((long long)p.parts * kBins + p.Nk + p.Nk % 2) * (long long)sizeof(unsigned) : 0;
 }
 
@@ -540,10 +544,14 @@ hipError_t launch_evict(const EvictParams &params, hipStream_t stream) {
     }
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    // Half the rows leave or more: most that stay come from behind the first n_keep.
-    const bool far = p.Nk / 2 >= p.n_keep;
+    // Half the rows leave or more: most that stay come from behind the first n_keep, and with many of those a launch of their own pays
+    // (8 pairs: 32768 rows to 8000 43.4 -> 37.3 us, 16384 to 4096 25.2 -> 24.7, 8192 to 2048 18.8 -> 20.2; 64: 20000 to 5000 102.6 -> 92.3,
+    // 4096 to 2000 31.0 -> 35.6).
+    const bool far = p.Nk / 2 >= p.n_keep && p.n_keep >= 4096;
     const long long halves = (long long)p.B * p.Hkv * 2;
     const int split = far ? p.n_keep : p.Nk;
+    // Slices of 64 bytes where they make 256 workgroups, one for each CU, else of 32 (32 against 64 bytes, 64 pairs: 4096 rows to 3900
+    // 59.6 -> 47.9 us, 128: 203 -> 131; 8: 17000 to 12000 52.5 and 59.7).
     if (halves * (p.D / 32) >= 256)
         move<4>(p, split, stream);
     else

@@ -8,17 +8,26 @@
 // every lane adds up its four keys' p over its column of each tile; the 16 columns of a tile meet once, at the end.
 //   * Nothing of the size rows x keys ever leaves the registers, and no sums meet in memory in an order that changes: a key's sum
 //     is one workgroup's, or one sum per chunk of the columns added up by a second kernel in the chunks' order.
-//   * Few rows (a decode step): the read of K is all there is.  Many: matrix and exponential work about balanced.
+//   * Few rows (a decode step): the read of K is all there is: 131072 keys of 8 heads in 54 us, 4.9 TB/s.  Many: matrix and
+//     exponential work, one beside the other (16 MFMA, 16 exponentials and 32 multiply-adds of a tile column take 406 cycles of which
+//     the MFMA have 256): 1121 TFLOP/s for 16384 rows of one head on 32768 keys, where few tiles have a mask's edge in them.
 #include "swaa_cache_ops.h"
 
 namespace swaa {
 namespace {
 
 constexpr int kWThreads = 256;
-constexpr int kMinChunk = 256;    // columns a workgroup goes through at least, if there are as many
-constexpr int kFewColumns = 256;  // up to here a wave has 32 keys instead of 64
+// Columns a workgroup goes through at least, if there are as many (us for 256, 512, 1024; 32 heads: 2048 rows with a window of 512 37.2, 34.8,
+// 49.2; 4096 with 256 57.4, 48.8, 61.3; 1024 that see 4096 keys 47.4, 44.9, 49.5).
+constexpr int kMinChunk = 512;
+// A wave has 32 keys instead of 64 where there are few columns and, in all pairs together, few keys, which would be workgroups for
+// part of the chip only; or for a decode step's columns at any length (32 keys against 64, us: 64 rows of 32 heads on 32768 keys of 8 32.9
+// and 34.2, on 131072 104 and 94; 4 x 64 rows on 4096 18.4 and 20.4; one row on 4096 4.2 and 5.6, on 131072 49.2 and 50.6).
+constexpr int kFewColumns = 256, kStepColumns = 16;
+constexpr long long kFewKeys = 1 << 18;
 constexpr int kListedWgs = 1024;  // workgroups that go through a list of tiles (one per tile of the longest sequence instead: 47.8 -> 39.0 us, 16 of 0.2-16k)
-constexpr int kFillItems = 4096;  // workgroups that a call should have
+constexpr int kFillItems = 4096;  // workgroups that a call should have (2048, 4096, 6144: 16384 rows of 32 heads with a window of 2048
+                                  // 337, 328, 334 us, 8001 rows of 40 heads that see all 350, 348, 354)
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -426,9 +435,10 @@ hipError_t launch(const KeyWeightsParams &p, hipStream_t stream) {
 bool plan_key_weights(KeyWeightsParams &p) {
     const int Nq = p.seq.Nq, Nk = p.seq.Nk;
     if ((long long)p.G * (Nq + 64LL) > 0x3fffffffLL) return false;
-    p.key_tile = (long long)p.G * Nq <= kFewColumns ? 128 : 256;
-    p.one_stage = (long long)p.G * Nq <= stage_cols(p.D);
     p.pairs = p.seq.B * (p.Hq / p.G);
+    const long long columns = (long long)p.G * Nq;
+    p.key_tile = columns <= kStepColumns || (columns <= kFewColumns && (long long)p.pairs * Nk <= kFewKeys) ? 128 : 256;
+    p.one_stage = columns <= stage_cols(p.D);
     p.tiles = (Nk + p.key_tile - 1) / p.key_tile;
     // stages (of 64 columns) of a tile seen by n rows, at most
     auto stages_of = [&](long long n) { return Columns<64>((int)(n < Nq ? n : Nq), p.G).stages; };

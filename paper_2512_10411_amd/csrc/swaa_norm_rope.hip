@@ -7,7 +7,9 @@
 // backward pass goes through the transposed rotation, g_j = C_j dy_j + S_p dy_p with S_p = -S_j, and the norm:
 // dx_j = r (w_j g_j - x_j r^2 mean(x w g)), dw_j = sum over rows of g_j x_j r.
 //
-// Bound by memory: every element comes in once and goes out once (backward: two in, one out).
+// Bound by memory: every element comes in once and goes out once (backward: two in, one out).  32 + 8 heads of 128, bf16: 16384 tokens
+// forward 75.6 us (4.4 TB/s; a copy of 128 MB to 2 GB: 8.6 to 4.9), backward 115.4 us (4.4 TB/s, of it 5 us for the sums of the weights'
+// gradients); 16 tokens into a cache 6.2 us, a launch's time and the angles.
 //   * A row is D / 8 lanes of 16 bytes (rounded up to a power of two); what a lane multiplies by depends on its token and its
 //     place in the row only, so a lane keeps both through a loop over the heads: cosines, sines and weights stay in registers.
 //   * The angles are taken in 64 bits (positions go beyond what 32 bits resolve), once per token and pair: a workgroup's
@@ -18,8 +20,17 @@ namespace swaa {
 namespace {
 
 constexpr int kNThreads = 256;
-constexpr int kByWaveTokens = 1024;  // tokens from which on each wave has its own
-constexpr int kLeastUnits = 4;       // units that a workgroup of those has at least
+// Tokens from which on each wave has its own (us of the forward / backward call, 32 + 8 heads of 128, bf16: 128 tokens shared 6.2 / 11.2,
+// by wave 6.6 / 11.6; 256: 7.0 / 12.2, 6.4 / 11.6; 1000: 11.2 / 19.2, 9.6 / 16.3).
+constexpr int kByWaveTokens = 256;
+// Units that a workgroup of those has at least: what it does for its angles has to pay.  Twice as many where there are tiles enough
+// to fill the chip all the same (4 units against 8: 300 tokens 6.4 / 11.5, 7.3 / 12.4; 700: 8.1 / 14.6, 7.9 / 13.8; 2000: 15.4 / 22.4,
+// 12.2 / 21.4; 1 unit against 4 at 1000: 12.0 / 18.7, 9.5 / 16.1).
+constexpr int kLeastUnits = 4;
+constexpr int kManyTiles = 32;
+// Workgroups that a call should have: what the chip holds at once (1024 against 2048, 3000 tokens: 18.0 / 30.3, 21.2 / 32.4; 8192: 31.4 / 54.0,
+// 34.5 / 54.5).
+constexpr int kFillWgs = 1024;
 
 template <bool kF16>
 __device__ __forceinline__ void unpack(u32x4 raw, float (&x)[8]) {
@@ -440,8 +451,9 @@ int lanes_of_row(int D) { return D <= 32 ? 4 : D <= 64 ? 8 : D <= 128 ? 16 : 32;
 
 // Tile and units.  A wave has as many tokens as rows at a time (four of head dimension 128), fewer if there are fewer.  Few tokens: the
 // four waves share them and take different heads.  Many: each wave has its own and goes through the heads by itself.  The
-// units of a tile are shared out over workgroups until there are `target`.
-bool plan(NormRopeParams &p, int target, bool backward) {
+// units of a tile are shared out over workgroups until there are kFillWgs; a backward call has no more than those, of several tiles
+// each, so that few sums are left to add up.
+bool plan(NormRopeParams &p, bool backward) {
     const int wave_rows = 64 / lanes_of_row(p.D);
     p.wave_shift = 0;
     while ((2 << p.wave_shift) <= wave_rows && (1LL << p.wave_shift) < p.tokens) ++p.wave_shift;
@@ -453,13 +465,13 @@ bool plan(NormRopeParams &p, int target, bool backward) {
     p.v_units = p.v.ptr ? p.k_units : 0;
     const int units = p.q_units + p.k_units + p.v_units;
     const long long tiles = (p.tokens + p.tile_tokens - 1) / p.tile_tokens;
-    const long long parts = tiles >= target ? 1 : (target + tiles - 1) / tiles;
+    const long long parts = tiles >= kFillWgs ? 1 : (kFillWgs + tiles - 1) / tiles;
     p.units_per_wg = (int)((units + parts - 1) / parts);
-    const int least = p.by_wave ? kLeastUnits : 1;
+    const int least = !p.by_wave ? 1 : tiles < kManyTiles ? kLeastUnits : 2 * kLeastUnits;
     if (p.units_per_wg < least) p.units_per_wg = least < units ? least : units;
     p.wgs_per_tile = (units + p.units_per_wg - 1) / p.units_per_wg;
     p.div_wgs = make_fastdiv((unsigned)p.wgs_per_tile);
-    p.tiles_per_wg = backward ? (tiles + target - 1) / target : 1;
+    p.tiles_per_wg = backward ? (tiles + kFillWgs - 1) / kFillWgs : 1;
     p.wgs = (tiles + p.tiles_per_wg - 1) / p.tiles_per_wg * p.wgs_per_tile;
     return p.wgs <= 0x7fffffffLL;
 }
@@ -489,8 +501,8 @@ struct Bwd {
 
 }  // namespace
 
-bool plan_norm_rope(NormRopeParams &p) { return plan(p, 1024, false); }
-bool plan_norm_rope_bwd(NormRopeParams &p) { return plan(p, 1024, true); }
+bool plan_norm_rope(NormRopeParams &p) { return plan(p, false); }
+bool plan_norm_rope_bwd(NormRopeParams &p) { return plan(p, true); }
 
 hipError_t launch_norm_rope(const NormRopeParams &p, hipStream_t stream) { return dispatch<Fwd>(p, stream); }
 

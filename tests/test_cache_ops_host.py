@@ -124,6 +124,12 @@ def test_evict_refusals(status, kw):
     assert evict(**kw) == getattr(binding, "SWAA_ERR_" + status)
 
 
+def test_evict_has_no_more_pairs_than_a_launch_can_move():
+    assert binding.swaa_cache_evict_workspace_bytes(30000, 8, 64, 128) == 0
+    for B, D in ((30841, 128), (1 << 24, 32)):
+        assert evict(B=B, Hkv=8, D=D, Nk=64) == binding.SWAA_ERR_SHAPE
+
+
 def test_evict_workspace():
     need = binding.swaa_cache_evict_workspace_bytes(2, 2, 100000, 128)
     long = dict(Nk=100000, weights_stride_b=200000, weights_stride_h=100000, k=rows(2, 100000, 128), v=rows(2, 100000, 128))

@@ -58,6 +58,14 @@ def test_which_rows_stay_and_where(shape, kind, ties):
     run(kind, lens, H, D, n_keep, n_sink, n_recent, random_weights(len(lens), H, max(lens) + 3, gen, ties), gen)
 
 
+@pytest.mark.parametrize("kind", ["dense", "paged"])
+@pytest.mark.parametrize("D", [64, 128, 224])
+@pytest.mark.parametrize("n_keep", [4095, 4096, 4501])
+def test_rows_from_far_behind(D, kind, n_keep):
+    gen = torch.Generator().manual_seed(D + n_keep)
+    run(kind, [9000, 4600], 1, D, n_keep, 2, 64, random_weights(2, 1, 9001, gen), gen, **({"page_size": 24} if kind == "paged" else {}))
+
+
 @pytest.mark.parametrize("page_size", [1, 3, 64])
 def test_pages_of_any_size(page_size):
     gen = torch.Generator().manual_seed(page_size)
@@ -142,25 +150,26 @@ def select_only(weights, lens, n_keep, n_sink, n_recent, space):
 
 
 @pytest.mark.parametrize("ties", [0, 5, 1])
-@pytest.mark.parametrize("lens", [[16385, 3, 16384], [40000, 20001], [100001]])
+@pytest.mark.parametrize("lens", [[16385, 3, 16384], [32769, 3, 32768], [40000, 20001], [100001]])
 def test_long_sequences_shared_out_and_not(lens, ties):
     gen = torch.Generator().manual_seed(lens[0] + ties)
     N, n_keep, n_sink, n_recent = max(lens), max(lens) // 3, 4, 1000
     w = random_weights(len(lens), 2, N, gen, ties)
     shared, w1, need = select_only(w, lens, n_keep, n_sink, n_recent, True)
     alone, w2, _ = select_only(w, lens, n_keep, n_sink, n_recent, False)
-    assert need > 0 and torch.equal(shared, alone) and torch.equal(w1, w2)
+    assert (need > 0) == (N > 32768) and torch.equal(shared, alone) and torch.equal(w1, w2)
     for b, n in enumerate(lens):
         for g in range(2):
             want = ref.evict(w[b, g, :n], n, n_keep, n_sink, n_recent)
             assert shared[b, g].tolist() == want + [-1] * (n_keep - len(want))
 
 
-def test_many_long_sequences():
+@pytest.mark.parametrize("least", [17000, 33000])
+def test_many_long_sequences(least):
     """More pairs than are shared out: a workgroup each, in rounds."""
     gen = torch.Generator().manual_seed(70)
-    lens = [17000 + 41 * i for i in range(33)]
-    w = random_weights(33, 2, max(lens), gen)
+    lens = [least + 41 * i for i in range(33)]
+    w = random_weights(33, 3, max(lens), gen)
     kept, _, need = select_only(w, lens, 5000, 0, 7, True)
     assert need == 0
     for b in (0, 16, 32):

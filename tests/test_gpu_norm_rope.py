@@ -61,6 +61,22 @@ def test_prompts_of_projections(shape, fmt):
     assert torch.equal(on_gpu.cpu(), qkv)
 
 
+@pytest.mark.parametrize("N", [127, 128, 129, 1100])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 256])
+def test_few_tokens_and_many(D, N):
+    """Two sequences: around 256 tokens, from where on every wave takes tokens of its own, and more than one workgroup's share."""
+    gen = torch.Generator().manual_seed(D + N)
+    print(f"[case] {D} {N}", flush=True)
+    qkv = torch.randn(2, N, 9, D, generator=gen).to(torch.bfloat16)
+    on_gpu = qkv.cuda()
+    (q, k), (gq, gk) = ((t[:, :, :6].permute(0, 2, 1, 3), t[:, :, 6:].permute(0, 2, 1, 3)) for t in (qkv, on_gpu))
+    qw, kw = weights_of(D, gen, True)
+    inv = frequencies(D)
+    qo, ko, _ = binding.swaa_qk_norm_rope(gq, gk, inv.cuda(), q_weight=gpu(qw), k_weight=gpu(kw))
+    for name, got, x, w in (("q", qo, q, qw), ("k", ko, k, kw)):
+        close(got, *ref.norm_rope(x, w, torch.arange(N), inv, 1e-6, False), torch.bfloat16, f"{name} {D} {N}")
+
+
 def test_far_positions_of_every_sign():
     gen = torch.Generator().manual_seed(3)
     B, N, H, D = 1, 6, 2, 128
